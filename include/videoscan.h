@@ -50,6 +50,11 @@ extern "C" {
 #define VS_MAX_BATCH           64   /* most streams one call may list                       */
 #define VS_N_KERNEL_CLASSES    10   /* kernel classes reported by vs_profile_read           */
 #define VS_STATIC_MAX_BANK   4096   /* most carriers vs_evict_choose_static can score       */
+#define VS_MAX_AXES             4   /* most position axes of vs_rope_axes                   */
+#define VS_MAX_TOP             32   /* most alternatives vs_token_logprobs reports          */
+#define VS_CACHE_PAGE          64   /* tokens a page of the paged cache holds               */
+#define VS_CACHE_MAX_SEQS    1024   /* most sequences a call on the paged cache can list    */
+#define VS_CACHE_MAX_HEADS    256   /* most KV heads of a paged cache                       */
 
 typedef struct vs_stream vs_stream;   /* opaque handle: a batch of n_streams independent video streams */
 
@@ -283,6 +288,114 @@ int vs_evict_choose_static(const void* bank_emb, const void* incoming, int32_t c
                            int32_t policy, int32_t* victim_out, void* cuda_stream);
 
 int vs_destroy_stream(vs_stream* h);
+
+/* ---- Stand-alone operators: frames kept in detail ---------------------------------------------
+ * The bank keeps one carrier a frame.  A program that also keeps some frames, or all of them, with
+ * every visual token (the systems the paper compares with do, Section 4.2) finds here what that
+ * takes: rotary positions with several axes, a paged cache of 8-bit keys and values, attention over
+ * it; and, beside vs_lm_head, what the logits say about given tokens.
+ * These calls need no handle: the device is an argument (made current for the call and put back),
+ * and they only enqueue work on `cuda_stream`, which must belong to it.  They keep nothing between
+ * calls, allocate nothing, and may be captured into a graph; calls on different streams are
+ * independent unless they share a workspace or write the same memory.  Integer arrays marked DEVICE
+ * are read when the kernels run, so a captured call follows what they hold then.  Strides are in
+ * elements; `dtype`: 0 = bf16, 1 = fp32. */
+
+/* Rotary positions with several axes (a video token's time, height, width): for pair k of a head,
+ *   (y_k, y_{k + D/2}) = (x_k cos t - x_{k + D/2} sin t,  x_{k + D/2} cos t + x_k sin t),
+ *   t = positions[axis(k)][row] * theta^(-2k / D);
+ * inverse != 0 turns back by the same angle (which is also the gradient with respect to x).
+ * sections: HOST [n_axes], pairs of each axis (may be 0), their sum D/2.  interleaved = 0: the axes'
+ * pairs one axis after the other; 1: the pairs dealt to the axes in turn, an axis that has its share
+ * left out of the later rounds.  One axis: the rotation that vs_frame_prefill applies.
+ * x, out: DEVICE [rows][heads][head_dim] of dtype, 16-byte aligned, strides multiples of 16 bytes,
+ *   the head_dim elements side by side; out may be x itself (same strides), but must not overlap it otherwise.
+ * positions: DEVICE int64 [n_axes][rows], pos_stride between axes; |position| < 2^31 keeps the angle
+ *   exact to 1e-6.
+ * head_dim: a multiple of 16 up to 256.  n_axes: 1 .. VS_MAX_AXES. */
+int vs_rope_axes(const void* x, int64_t x_row_stride, int64_t x_head_stride,
+                 void* out, int64_t out_row_stride, int64_t out_head_stride, int32_t dtype,
+                 int32_t rows, int32_t heads, int32_t head_dim,
+                 const int64_t* positions, int64_t pos_stride, int32_t n_axes, const int32_t* sections,
+                 int32_t interleaved, int32_t inverse, double theta, int32_t device, void* cuda_stream);
+
+/* A paged cache of 8-bit keys and values, the caller's memory.  Codes are e4m3 (largest 448); a
+ * page's codes of one head share a scale 2^e, e in [-110, 120]: value = code * 2^e, exact in bf16. */
+typedef struct {
+  void*  k;                      /* DEVICE e4m3 [n_pages][n_kv_heads][VS_CACHE_PAGE][head_dim], 16-byte aligned */
+  void*  v;                      /* ... values                                                       */
+  float* k_scale;                /* DEVICE fp32 [n_pages][n_kv_heads]                                */
+  float* v_scale;
+  int32_t n_pages;
+  int32_t n_kv_heads;            /* 1 .. VS_CACHE_MAX_HEADS                                          */
+  int32_t head_dim;              /* 64 or 128                                                        */
+  int32_t device;                /* CUDA device ordinal                                              */
+} vs_cache;
+
+/* The sequences of a call and its packed rows: sequence i has rows row_offsets[i] .. row_offsets[i + 1] - 1.
+ * Token t of a sequence lies in row t % 64 of page page_table[i][t / 64].  An entry outside [0, n_pages),
+ * or beyond table_width, is no page: rows are not written to it, read as zeros, and its keys are not seen. */
+typedef struct {
+  const int32_t* page_table;     /* DEVICE [n_seqs][table_width]                                     */
+  const int32_t* tokens;         /* DEVICE [n_seqs]; write, read: place of the sequence's first row (the tokens
+                                    ahead of it); attention: tokens of the sequence, the call's rows counted in */
+  const int32_t* row_offsets;    /* DEVICE [n_seqs + 1], ascending from 0 to n_rows; NULL: n_rows / n_seqs rows each */
+  int32_t n_seqs;                /* 1 .. VS_CACHE_MAX_SEQS                                           */
+  int32_t table_width;
+  int32_t n_rows;                /* rows of the call, all sequences                                  */
+  int32_t reserved;              /* 0                                                                */
+} vs_cache_rows;
+
+/* Appends rows to sequences, quantising them: a page's scale is the smallest power of two with every
+ * finite magnitude written to it at most 448 of it, and not below the scale that the page had for the tokens
+ * ahead of the rows; where rows raise it, the codes of those tokens are rounded once more at the new scale.  A row written to
+ * the first place of a page starts the page afresh.  Nearest code, ties to even; infinities become +-448, NaN stays
+ * NaN.  Appending ends the sequence: codes behind its last row are left as they were and count for nothing.
+ * k, v: DEVICE [n_rows][n_kv_heads][head_dim] of dtype, 16-byte aligned, strides multiples of 16 bytes.
+ * No page may be written for two sequences of a call (pages that several sequences share must be full);
+ * which of them is kept is not defined then. */
+int vs_cache_write(const vs_cache* cache, const vs_cache_rows* rows,
+                   const void* k, int64_t k_row_stride, int64_t k_head_stride,
+                   const void* v, int64_t v_row_stride, int64_t v_head_stride, int32_t dtype, void* cuda_stream);
+
+/* Reads rows back: the values that the codes stand for, exact in either dtype. */
+int vs_cache_read(const vs_cache* cache, const vs_cache_rows* rows,
+                  void* k, int64_t k_row_stride, int64_t k_head_stride,
+                  void* v, int64_t v_row_stride, int64_t v_head_stride, int32_t dtype, void* cuda_stream);
+
+/* Softmax attention of each sequence's rows over its tokens in the cache (Eq. 1, grouped KV heads):
+ * row j of n stands at position tokens - n + j and sees the tokens that exist, with causal != 0 none
+ * behind itself, with window > 0 only the last `window` up to itself.  A row that sees nothing gets zeros
+ * (and -inf in lse).  Tokens that no row of the call sees may hold anything.
+ * q:   DEVICE bf16 [n_rows][n_q_heads][head_dim], 16-byte aligned, strides multiples of 8;
+ *      n_q_heads % n_kv_heads == 0, at most 8 query heads a KV head.
+ * out: DEVICE [n_rows][n_q_heads][head_dim] of out_dtype, 8-byte (bf16) or 16-byte (fp32) aligned,
+ *      strides multiples of 4.  Softmax weights are rounded to 11 bits, sums are fp32.
+ * lse: DEVICE fp32 [n_rows][n_q_heads], log sum exp of a row's scores, or NULL: what joining the rows
+ *      with those over other keys (the bank's, say) takes.
+ * scale: of the scores, usually 1 / sqrt(head_dim).
+ * workspace: DEVICE, at least vs_cache_attention_bytes, 256-byte aligned; its contents need not be kept
+ *      between calls, but no two calls that may overlap can share it. */
+int vs_cache_attention_bytes(int32_t head_dim, size_t* out_bytes);
+int vs_cache_attention(const vs_cache* cache, const vs_cache_rows* rows,
+                       const void* q, int64_t q_row_stride, int64_t q_head_stride, int32_t n_q_heads,
+                       float scale, int32_t causal, int32_t window,
+                       void* out, int64_t out_row_stride, int64_t out_head_stride, int32_t out_dtype,
+                       float* lse, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/* What rows of logits (vs_lm_head's) say about given tokens:
+ *   logprob[r] = x_t - log sum_j e^{x_j}, t = tokens[r];  entropy[r] = -sum_j p_j log p_j (nats);
+ *   rank[r] = how many tokens come before t in the order "larger logit, else lower index, NaN below every
+ *   number" (0: t is vs_lm_head's next_token);  top_index, top_logprob [rows][top]: the first `top` of that order.
+ * logits: DEVICE [rows][vocab] of dtype, row_stride between rows, aligned to their type (faster when rows
+ *   begin on 16-byte boundaries); -inf is a token that cannot be.
+ * tokens: DEVICE int32 [rows]; a negative one asks nothing (logprob 0, rank -1), one >= vocab gets NaN and -1.
+ * Outputs: DEVICE, each may be NULL (top_index not when top > 0); all fp32 but rank and top_index (int32).
+ * A row that holds NaN or +inf has NaN for what is summed; one of -inf only has -inf and entropy 0.
+ * top: 0 .. VS_MAX_TOP, at most vocab. */
+int vs_token_logprobs(const void* logits, int64_t row_stride, int32_t dtype, int32_t rows, int32_t vocab,
+                      const int32_t* tokens, int32_t top, float* logprob, float* entropy, int32_t* rank,
+                      int32_t* top_index, float* top_logprob, int32_t device, void* cuda_stream);
 
 const char* vs_status_string(int status);
 

@@ -1,0 +1,470 @@
+// vs_cache_attention: softmax attention over a paged cache of 8-bit keys and values.  Here: the call, the kernel for sequences of few
+// rows (an answer's token), and the kernel that joins what several CTAs worked out of the same rows.
+//
+//   o = sum_j w_j v_j / sum_j w_j,   w_j = e^{scale q k_j},   k_j = 2^{ek} * code, v_j = 2^{ev} * code  (a page's and head's own exponents)
+//
+// Codes go to the tensor cores as fp16, which holds every e4m3 value exactly; a page's exponents are applied to scores and weights, never
+// to the codes.  Scores are s = f (q' code) with q' the query row times a power of two that brings its largest magnitude to 2^14 .. 2^15
+// (bf16 values are then exact in fp16 down to 2^-39 of that) and f the rest of the scale.  With x = s + ev, in the log2 domain, and m the running maximum of x:
+//   O += 2^{x - m + 15} code_v,   l += 2^{x - m + 15} 2^{-ev},   o = O / l:
+// the reference goes by what a key adds to the output, so pages of different exponents need no rescaling between them.  Weights are
+// rounded to fp16 (a half step, 2^-12 relative; the smallest, 2^-40 of the largest, is far below any sum's last bit); maxima, sums and rows are fp32.
+//
+// What bounds the few-row kernel: the codes' bytes, once from HBM.  All heads of a KV group, and a few tokens, are the 8 (or 16)
+// columns of mma.sync: S^T = K q^T and O^T += V^T P^T, 16 keys a step, so a page is read once for the whole group; a tcgen05 tile of 128
+// rows would hold 7.  A CTA is four warps, each with 16 keys of a page in a ring of its own, filled by 16-byte asynchronous copies
+// kStages - 1 pages ahead and placed so that both operands' fragments are read without bank conflicts: no barrier in the loop.
+// The work of all sequences is cut into equal runs of pages (count_units): long and short sequences side by side leave no CTA idle.
+#include "vs_cache_attention.cuh"
+#include "vs_ptx.cuh"
+
+namespace vs {
+
+namespace {
+
+constexpr int kWarps = 4, kThreads = 32 * kWarps, kWarpKeys = kPage / kWarps, kStages = 4;
+constexpr float kLift = 15.f;
+
+__device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t half2_of(float lo, float hi) {
+  const __half2 h = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ uint4 lds128(uint32_t addr) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ uint2 lds64(uint32_t addr) {
+  uint2 v;
+  asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(addr) : "memory");
+  return v;
+}
+
+template <int D, int NT>
+struct Few {
+  static constexpr int W = 8 * NT;
+  static constexpr int kTile = kWarpKeys * D;                      // a warp's keys (or values) of a page, bytes
+  static constexpr int kStage = 2 * kTile;
+  static constexpr int kRing = kWarps * kStages * kStage;
+  static constexpr int kRowF = D + 4;                              // (a warp's rows, at the end of an item, lie in the ring)
+  static_assert(kWarps * W * (kRowF + 2) * 4 <= kRing, "rows of the four warps");
+  static constexpr int kMeta = kRing;                              // [warp][stage] (scale of K, scale of V)
+  static constexpr int kBefore = kMeta + kWarps * kStages * 8;     // units ahead of each sequence
+  static int bytes(int n_seqs) { return kBefore + 8 * (n_seqs + 1); }
+};
+
+// Places of a 16-byte piece c of row r (0..15): keys are read by quads of lanes, eight rows side by side; values by eight lanes of one
+// piece each, rows 2 q apart.  The exclusive or spreads either over all banks.
+__device__ __forceinline__ uint32_t k_place(int r, int c, int D) { return (uint32_t)(r * D + ((D == 128 ? c ^ ((r & 1) << 2) : c) << 4)); }
+__device__ __forceinline__ uint32_t v_place(int r, int c, int D) { return (uint32_t)(r * D + ((D == 128 ? c ^ (r & 6) : c) << 4)); }
+
+template <int D, int NT>
+__global__ void __launch_bounds__(kThreads) cache_attention_few_kernel(const __grid_constant__ CacheAttnArgs a) {
+  using F = Few<D, NT>;
+  constexpr int W = F::W, KS = D / 16, CPR = D / 16;               // k-steps of a score; 16-byte pieces of a row
+  extern __shared__ __align__(128) uint8_t smem[];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, q4 = lane & 3;
+  long long* before = reinterpret_cast<long long*>(smem + F::kBefore);
+  pdl_launch_dependents();
+  const long long units = count_units<W>(a, before);
+  const int n_ctas = ctas_at_work(a, units, (int)gridDim.x), cta = (int)blockIdx.x;
+  if (tid == 0) a.joins[cta] = make_int4(0, 0, 0, 0);
+  if (cta >= n_ctas || units == 0) return;
+  const long long u_begin = run_begin(units, n_ctas, cta), u_end = run_begin(units, n_ctas, cta + 1);
+  const uint32_t ring = smem_u32(smem) + (uint32_t)(warp * kStages * F::kStage);
+  float2* meta = reinterpret_cast<float2*>(smem + F::kMeta) + warp * kStages;
+
+  for (long long u = u_begin; u < u_end;) {
+    const AttnItem it = item_at<W>(a, before, u, u_end);
+    if (it.n < 1) break;             // (only if the sequences changed under the kernel)
+    const SeqShape s = shape_of<W>(a, it.seq);
+    u += it.n;
+    const int r0 = it.tile * W, n_cols = (int)min((long long)W, (long long)s.n * a.G - r0);
+
+    // ---- pages on their way ---------------------------------------------------------------------------------
+    auto load_page = [&](int i) {
+      if (i < it.n) {
+        const int page = page_of(a.r, a.c.n_pages, it.seq, it.page + i);
+        const size_t tile = (size_t)max(page, 0) * a.c.n_kv_heads + it.head;
+        const uint8_t* k = static_cast<const uint8_t*>(a.c.k) + tile * (kPage * D) + warp * F::kTile;
+        const uint8_t* v = static_cast<const uint8_t*>(a.c.v) + tile * (kPage * D) + warp * F::kTile;
+        const uint32_t at = ring + (uint32_t)((i % kStages) * F::kStage);
+#pragma unroll
+        for (int j = 0; j < F::kTile / 512; ++j) {
+          const int p = j * 32 + lane, r = p / CPR, c = p % CPR;
+          cp_async16(at + k_place(r, c, D), k + p * 16, page >= 0);
+          cp_async16(at + (uint32_t)F::kTile + v_place(r, c, D), v + p * 16, page >= 0);
+        }
+        // (a page that is not there: a negative scale, which no page has)
+        if (lane == 0) meta[i % kStages] = page >= 0 ? make_float2(a.c.k_scale[tile], a.c.v_scale[tile]) : make_float2(-1.f, 1.f);
+      }
+      cp_async_commit();
+    };
+    __syncthreads();                 // the rows of the item before, in the ring, have been read
+#pragma unroll
+    for (int i = 0; i < kStages - 1; ++i) load_page(i);
+
+    // ---- the query: column n of a B operand, 16 (q4 + 4 i) + 4 w + e of the row in k-step 4 i + w --------------------
+    uint32_t qf[NT][KS][2];
+    float factor[NT][2];             // of the columns 2 q4, 2 q4 + 1 that the lane has scores of
+    int hi_of[NT][2], lo_of[NT][2];  // keys that they see
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      const int col = 8 * n + g, r = r0 + min(col, n_cols - 1), t = r / a.G, h = it.head * a.G + (r - t * a.G);
+      const bf16* row = a.q + (long long)(s.first + t) * a.q_row + (long long)h * a.q_head;
+      uint4 raw[KS / 4][2];
+      float amax = 0.f;
+#pragma unroll
+      for (int i = 0; i < KS / 4; ++i) {
+        raw[i][0] = *reinterpret_cast<const uint4*>(row + 16 * (q4 + 4 * i));
+        raw[i][1] = *reinterpret_cast<const uint4*>(row + 16 * (q4 + 4 * i) + 8);
+#pragma unroll
+        for (int w = 0; w < 8; ++w) {
+          const uint32_t two = word(raw[i][w >> 2], w & 3);
+          const float x = fabsf(__uint_as_float(two << 16)), y = fabsf(__uint_as_float(two & 0xffff0000u));
+          amax = fmaxf(amax, fmaxf(x <= 3.402823466e38f ? x : 0.f, y <= 3.402823466e38f ? y : 0.f));
+        }
+      }
+      amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
+      amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
+      const int e = max(exponent_of(amax), -100) - 14;
+      const float up = power_of_two(-e), back = power_of_two(e) * a.scale_log2e;
+#pragma unroll
+      for (int i = 0; i < KS / 4; ++i)
+#pragma unroll
+        for (int w = 0; w < 8; ++w) {
+          const uint32_t two = word(raw[i][w >> 2], w & 3);
+          qf[n][4 * i + (w >> 1)][w & 1] = half2_of(__uint_as_float(two << 16) * up, __uint_as_float(two & 0xffff0000u) * up);
+        }
+      const KeyRange seen = keys_of(a, s, t);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int from = (2 * q4 + j) * 4;                       // a lane of that column
+        factor[n][j] = __shfl_sync(0xffffffffu, back, from);
+        hi_of[n][j] = __shfl_sync(0xffffffffu, seen.hi, from);
+        lo_of[n][j] = __shfl_sync(0xffffffffu, seen.lo, from);
+      }
+    }
+    // keys that every column sees, and that any does
+    int all_lo = 0, all_hi = 0x7fffffff, any_hi = 0, any_lo = 0x7fffffff;
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        all_lo = max(all_lo, lo_of[n][j]); all_hi = min(all_hi, hi_of[n][j]);
+        any_lo = min(any_lo, lo_of[n][j]); any_hi = max(any_hi, hi_of[n][j]);
+      }
+    all_lo = __reduce_max_sync(0xffffffffu, all_lo); all_hi = __reduce_min_sync(0xffffffffu, all_hi);
+    any_lo = __reduce_min_sync(0xffffffffu, any_lo); any_hi = __reduce_max_sync(0xffffffffu, any_hi);
+
+    float o[NT][KS][4];              // O^T: tile m of 16 dims; rows g -> (D / 8) g + 2 m, g + 8 -> that + 1; columns 2 q4, 2 q4 + 1
+    float m_run[NT][2], l_run[NT][2];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+#pragma unroll
+      for (int i = 0; i < KS; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[n][i][j] = 0.f;
+      m_run[n][0] = m_run[n][1] = -INFINITY;
+      l_run[n][0] = l_run[n][1] = 0.f;
+    }
+
+    for (int i = 0; i < it.n; ++i) {
+      cp_async_wait<kStages - 2>();
+      __syncwarp();                  // this page is here, and every lane is done with the one before
+      load_page(i + kStages - 1);
+      const uint32_t at = ring + (uint32_t)((i % kStages) * F::kStage);
+      const float2 scales = meta[i % kStages];
+      const int key0 = (it.page + i) * kPage + warp * kWarpKeys;
+      const bool there = scales.x >= 0.f;
+      if (!there || key0 >= any_hi || key0 + kWarpKeys <= any_lo) continue;      // (the same for the whole warp)
+      // S^T = K q^T
+      float sc[NT][4];
+#pragma unroll
+      for (int n = 0; n < NT; ++n) sc[n][0] = sc[n][1] = sc[n][2] = sc[n][3] = 0.f;
+#pragma unroll
+      for (int h = 0; h < KS / 4; ++h) {
+        const uint4 ka = lds128(at + k_place(g, q4 + 4 * h, D)), kb = lds128(at + k_place(g + 8, q4 + 4 * h, D));
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          const uint32_t x = word(ka, w), y = word(kb, w);
+          const uint32_t a0 = codes_to_half2(x & 0xffffu), a2 = codes_to_half2(x >> 16), a1 = codes_to_half2(y & 0xffffu), a3 = codes_to_half2(y >> 16);
+#pragma unroll
+          for (int n = 0; n < NT; ++n) mma_f16(sc[n], a0, a1, a2, a3, qf[n][4 * h + w][0], qf[n][4 * h + w][1]);
+        }
+      }
+      const int ev = exponent_of(scales.y);
+      const float evf = (float)ev, down = power_of_two(-ev);
+      const bool edge = key0 < all_lo || key0 + kWarpKeys > all_hi;
+      uint32_t pf[NT][2];
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        float x[4], mx[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          x[j] = fmaf(sc[n][j], factor[n][j & 1] * scales.x, evf);
+          x[j] = x[j] == x[j] ? x[j] : INFINITY;                       // (NaN goes on as infinity - infinity)
+          const int key = key0 + g + 8 * (j >> 1);
+          if (edge && (key >= hi_of[n][j & 1] || key < lo_of[n][j & 1])) x[j] = -INFINITY;
+          mx[j & 1] = fmaxf(mx[j & 1], x[j]);
+        }
+        bool moved = false;
+        float r[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          mx[j] = fmaxf(mx[j], __shfl_xor_sync(0xffffffffu, mx[j], 4));
+          mx[j] = fmaxf(mx[j], __shfl_xor_sync(0xffffffffu, mx[j], 8));
+          mx[j] = fmaxf(mx[j], __shfl_xor_sync(0xffffffffu, mx[j], 16));
+          const float m = fmaxf(m_run[n][j], mx[j]);
+          moved = moved || m > m_run[n][j];
+          r[j] = m == -INFINITY ? 1.f : exp2f(m_run[n][j] - m);
+          m_run[n][j] = m;
+        }
+        if (__any_sync(0xffffffffu, moved)) {
+#pragma unroll
+          for (int j = 0; j < 2; ++j) l_run[n][j] *= r[j];
+#pragma unroll
+          for (int i2 = 0; i2 < KS; ++i2)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) o[n][i2][j] *= r[j & 1];
+        }
+        float p[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          p[j] = exp2f(x[j] - (m_run[n][j & 1] == -INFINITY ? 0.f : m_run[n][j & 1] - kLift));
+          l_run[n][j & 1] = fmaf(p[j], down, l_run[n][j & 1]);
+        }
+        pf[n][0] = transpose_8x8(half2_of(p[0], p[1]));
+        pf[n][1] = transpose_8x8(half2_of(p[2], p[3]));
+      }
+      // O^T += V^T P^T: the lane's piece of dims, keys 2 q4, 2 q4 + 1, 2 q4 + 8, 2 q4 + 9
+      uint32_t vw[4][D / 32];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int r = 2 * q4 + (j & 1) + 8 * (j >> 1);
+        if constexpr (D == 128) {
+          const uint4 v = lds128(at + (uint32_t)F::kTile + v_place(r, g, D));
+          vw[j][0] = v.x; vw[j][1] = v.y; vw[j][2] = v.z; vw[j][3] = v.w;
+        } else {
+          const uint2 v = lds64(at + (uint32_t)F::kTile + v_place(r, g >> 1, D) + 8u * (uint32_t)(g & 1));
+          vw[j][0] = v.x; vw[j][1] = v.y;
+        }
+        // what no row sees may be anything, NaN among it, which a weight of 0 does not stop
+        if (edge && (key0 + r >= any_hi || key0 + r < any_lo))
+#pragma unroll
+          for (int w = 0; w < D / 32; ++w) vw[j][w] = 0u;
+      }
+#pragma unroll
+      for (int w = 0; w < D / 32; ++w)
+#pragma unroll
+        for (int hh = 0; hh < 2; ++hh) {
+          // bytes 2 hh and 2 hh + 1 of the four keys' words
+          const uint32_t x = __byte_perm(vw[0][w], vw[1][w], hh ? 0x7362 : 0x5140), y = __byte_perm(vw[2][w], vw[3][w], hh ? 0x7362 : 0x5140);
+          const uint32_t a0 = codes_to_half2(x & 0xffffu), a1 = codes_to_half2(x >> 16), a2 = codes_to_half2(y & 0xffffu), a3 = codes_to_half2(y >> 16);
+#pragma unroll
+          for (int n = 0; n < NT; ++n) mma_f16(o[n][2 * w + hh], a0, a1, a2, a3, pf[n][0], pf[n][1]);
+        }
+    }
+    cp_async_wait<0>();
+    __syncthreads();                 // nobody reads the ring any more
+
+    // ---- the four warps' rows, joined --------------------------------------------------------------------------
+    float* rows = reinterpret_cast<float*>(smem);                  // [warp][column][kRowF], then [warp][column] (m, l)
+    float2* stats = reinterpret_cast<float2*>(rows + kWarps * W * F::kRowF);
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        float l = l_run[n][j];
+        l += __shfl_xor_sync(0xffffffffu, l, 4);
+        l += __shfl_xor_sync(0xffffffffu, l, 8);
+        l += __shfl_xor_sync(0xffffffffu, l, 16);
+        const int col = 8 * n + 2 * q4 + j;
+        if (g == 0) stats[warp * W + col] = make_float2(m_run[n][j], l);
+        float* row = rows + (warp * W + col) * F::kRowF + (D / 8) * g;
+#pragma unroll
+        for (int i = 0; i < KS; ++i) { row[2 * i] = o[n][i][j]; row[2 * i + 1] = o[n][i][j + 2]; }
+      }
+    __syncthreads();
+    const bool begun = it.page > it.first, goes_on = it.page + it.n < it.first + it.of;
+    float* part = nullptr;
+    if (begun || goes_on) part = part_rows<W, D>(a.parts, cta, begun ? 0 : 1);
+    for (int i = tid; i < n_cols * (D / 4); i += kThreads) {
+      const int col = i / (D / 4), d = (i - col * (D / 4)) * 4;
+      float m = -INFINITY;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) m = fmaxf(m, stats[w * W + col].x);
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+      float l = 0.f;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) {
+        const float2 st = stats[w * W + col];
+        const float f = st.x == -INFINITY ? 0.f : exp2f(st.x - m);
+        const float4 x = *reinterpret_cast<const float4*>(rows + (w * W + col) * F::kRowF + d);
+        v.x = fmaf(f, x.x, v.x); v.y = fmaf(f, x.y, v.y); v.z = fmaf(f, x.z, v.z); v.w = fmaf(f, x.w, v.w);
+        l = fmaf(f, st.y, l);
+      }
+      if (part != nullptr) {
+        *reinterpret_cast<float4*>(part + (size_t)col * D + d) = v;
+        if (d == 0) part_stats<W, D>(a.parts, cta, begun ? 0 : 1)[col] = make_float2(m - kLift, l);
+      } else {
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        store_row_piece(a, s.first, r0 + col, it.head, d, make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv));
+        if (d == 0) store_lse(a, s.first, r0 + col, it.head, m - kLift, l);
+      }
+    }
+    if (begun && !goes_on && tid == 0) {
+      const long long u_item = u - it.of;                          // the item's first unit
+      a.joins[cta] = make_int4(1 + cta_of(units, n_ctas, u_item), s.first, r0, it.head | (n_cols << 16));
+    }
+  }
+}
+
+// ---- rows that several CTAs worked on ------------------------------------------------------------------------------
+// A block a (CTA that was the last on its item, column): eight warps take the parts by turns, a lane four dims.
+constexpr int kJoinWarps = 8;
+template <int W, int D>
+__global__ void __launch_bounds__(32 * kJoinWarps) cache_attention_join_kernel(const __grid_constant__ CacheAttnArgs a) {
+  __shared__ float sm_m[kJoinWarps], sm_l[kJoinWarps];
+  __shared__ float4 sm_o[kJoinWarps][D / 4];
+  pdl_wait();
+  const int last = (int)blockIdx.x, col = (int)blockIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int4 j = a.joins[last];
+  if (j.x == 0 || col >= (j.w >> 16)) return;
+  const int first = j.x - 1;
+  float m = -INFINITY, l = 0.f;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  constexpr int U = 4;
+  for (int c0 = first + warp; c0 <= last; c0 += U * kJoinWarps) {
+    float2 st[U];
+    float4 v[U];
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const int c = c0 + i * kJoinWarps;
+      st[i] = make_float2(-INFINITY, 0.f);
+      v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (c <= last) {
+        const int place = c == first ? 1 : 0;
+        st[i] = part_stats<W, D>(a.parts, c, place)[col];
+        if (lane < D / 4) v[i] = *reinterpret_cast<const float4*>(part_rows<W, D>(a.parts, c, place) + (size_t)col * D + 4 * lane);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      if (st[i].x == -INFINITY) continue;
+      const float m_new = fmaxf(m, st[i].x), fa = m == -INFINITY ? 0.f : exp2f(m - m_new), fb = exp2f(st[i].x - m_new);
+      o.x = o.x * fa + v[i].x * fb; o.y = o.y * fa + v[i].y * fb; o.z = o.z * fa + v[i].z * fb; o.w = o.w * fa + v[i].w * fb;
+      l = l * fa + st[i].y * fb;
+      m = m_new;
+    }
+  }
+  if (lane == 0) { sm_m[warp] = m; sm_l[warp] = l; }
+  if (lane < D / 4) sm_o[warp][lane] = o;
+  __syncthreads();
+  if (warp != 0 || lane >= D / 4) return;
+  float M = -INFINITY;
+#pragma unroll
+  for (int w = 0; w < kJoinWarps; ++w) M = fmaxf(M, sm_m[w]);
+  float L = 0.f;
+  float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+  for (int w = 0; w < kJoinWarps; ++w) {
+    const float f = sm_m[w] == -INFINITY ? 0.f : exp2f(sm_m[w] - M);
+    const float4 x = sm_o[w][lane];
+    v.x += f * x.x; v.y += f * x.y; v.z += f * x.z; v.w += f * x.w;
+    L += f * sm_l[w];
+  }
+  const float inv = L == 0.f ? 0.f : 1.f / L;
+  store_row_piece(a, j.y, j.z + col, j.w & 0xffff, 4 * lane, make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv));
+  if (lane == 0) store_lse(a, j.y, j.z + col, j.w & 0xffff, M, L);
+}
+
+template <int D, int NT>
+int launch_few(const CacheAttnArgs& a, int ctas, cudaStream_t st) {
+  using F = Few<D, NT>;
+  const int bytes = F::bytes(a.r.n_seqs);
+  if (cudaFuncSetAttribute(cache_attention_few_kernel<D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return VS_ERR_CUDA;
+  cache_attention_few_kernel<D, NT><<<ctas, kThreads, bytes, st>>>(a);
+  return launched();
+}
+
+template <int W, int D>
+int launch_join(const CacheAttnArgs& a, int ctas, cudaStream_t st) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)ctas, (unsigned)W);
+  cfg.blockDim = dim3(32 * kJoinWarps);
+  cfg.stream = st;
+  cudaLaunchAttribute at = {};
+  at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &at;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, cache_attention_join_kernel<W, D>, a) == cudaSuccess ? launched() : VS_ERR_CUDA;
+}
+
+}  // namespace
+
+int launch_cache_attention_few(const CacheAttnArgs& a, int cols, int ctas, cudaStream_t st) {
+  if (cols <= 8) return a.c.head_dim == 128 ? launch_few<128, 1>(a, ctas, st) : launch_few<64, 1>(a, ctas, st);
+  return a.c.head_dim == 128 ? launch_few<128, 2>(a, ctas, st) : launch_few<64, 2>(a, ctas, st);
+}
+int launch_cache_attention_join(const CacheAttnArgs& a, int width, int ctas, cudaStream_t st) {
+  if (width == 8) return a.c.head_dim == 128 ? launch_join<8, 128>(a, ctas, st) : launch_join<8, 64>(a, ctas, st);
+  return a.c.head_dim == 128 ? launch_join<16, 128>(a, ctas, st) : launch_join<16, 64>(a, ctas, st);
+}
+
+}  // namespace vs
+
+namespace {
+constexpr int kFewCtas = 3 * 148, kFewMinPages = 4;
+constexpr size_t kJoinBytes = 16384;
+}
+
+extern "C" int vs_cache_attention_bytes(int32_t head_dim, size_t* out_bytes) {
+  if (out_bytes == nullptr) return VS_ERR_INVALID_ARG;
+  if (head_dim != 64 && head_dim != 128) return VS_ERR_UNSUPPORTED;
+  *out_bytes = kJoinBytes + (size_t)kFewCtas * 2 * 16 * (head_dim + 2) * 4;
+  return VS_OK;
+}
+
+extern "C" int vs_cache_attention(const vs_cache* cache, const vs_cache_rows* rows, const void* q, int64_t q_row_stride, int64_t q_head_stride,
+                                  int32_t n_q_heads, float scale, int32_t causal, int32_t window, void* out, int64_t out_row_stride,
+                                  int64_t out_head_stride, int32_t out_dtype, float* lse, void* workspace, size_t workspace_bytes,
+                                  void* cuda_stream) {
+  using namespace vs;
+  const int rc = check_cache(cache, rows);
+  if (rc != VS_OK) return rc;
+  if (n_q_heads < 1 || window < 0 || out_dtype < 0 || out_dtype > 1 || !(scale > 0.f) || !std::isfinite(scale)) return VS_ERR_INVALID_ARG;
+  if (n_q_heads % cache->n_kv_heads != 0 || n_q_heads / cache->n_kv_heads > 8) return VS_ERR_UNSUPPORTED;
+  const int G = n_q_heads / cache->n_kv_heads;
+  if (rows->n_rows > (1 << 27)) return VS_ERR_UNSUPPORTED;
+  size_t need = 0;
+  vs_cache_attention_bytes(cache->head_dim, &need);
+  if (rows->n_rows == 0) return VS_OK;
+  if (q == nullptr || out == nullptr || workspace == nullptr) return VS_ERR_INVALID_ARG;
+  if (workspace_bytes < need) return VS_ERR_CAPACITY;
+  if (!aligned(q, 16) || !aligned(out, out_dtype == 1 ? 16 : 8) || !aligned(workspace, 256) || !aligned(lse, 4)) return VS_ERR_INVALID_ARG;
+  if (q_row_stride % 8 != 0 || q_head_stride % 8 != 0 || out_row_stride % 4 != 0 || out_head_stride % 4 != 0) return VS_ERR_INVALID_ARG;
+  OnDevice on(cache->device);
+  if (!on.ok) return VS_ERR_CUDA;
+  CacheAttnArgs a = {};
+  a.c = *cache; a.r = *rows;
+  a.q = static_cast<const bf16*>(q); a.out = out; a.lse = lse;
+  a.joins = static_cast<int4*>(workspace);
+  a.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + kJoinBytes);
+  a.q_row = q_row_stride; a.q_head = q_head_stride; a.out_row = out_row_stride; a.out_head = out_head_stride;
+  a.scale_log2e = scale * 1.4426950408889634f;
+  a.Hq = n_q_heads; a.G = G; a.causal = causal != 0; a.window = window; a.out_fp32 = out_dtype;
+  a.min_pages = kFewMinPages;
+  a.few_cols = 0x7fffffff; a.take_few = 1;
+  const long long most = rows->row_offsets == nullptr ? (long long)(rows->n_rows / rows->n_seqs) * G : (long long)rows->n_rows * G;
+  const int cols = most <= 8 ? 8 : 16;
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  const int r1 = launch_cache_attention_few(a, cols, kFewCtas, st);
+  if (r1 != VS_OK) return r1;
+  return launch_cache_attention_join(a, cols, kFewCtas, st);
+}

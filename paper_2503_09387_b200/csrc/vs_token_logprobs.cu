@@ -1,0 +1,418 @@
+// vs_token_logprobs: what a row of logits says about a given token -- its log probability and its place in the order -- with the
+// entropy of the row and its best alternatives.
+//
+//   lse = log sum_j e^{x_j},   logprob = x_t - lse,   entropy = lse - sum_j p_j x_j,   p_j = e^{x_j - lse}
+//   rank = how many tokens come before t in the order "larger logit, else lower index"; alternatives: the first `top` of that order.
+//
+// One pass over the row with a running maximum m per thread:  s = sum of e^{x - m} over x < m,  c = how many x = m,
+// u = sum of (x - m) e^{x - m};  then log sum = log c + log1p(s / c) and entropy = that - u / (s + c).  (With the maxima counted and not
+// summed a row that is all but certain keeps the few bits that its entropy has.)
+// Alternatives: the k-th largest of the threads' own maxima is a bound that at least k logits reach, so only threads whose maximum reaches
+// it hold any of the best k.  Their logits -- a few dozen threads' -- are read once more (they lie in L2), those that reach the bound collected and put in
+// order by counting.
+//
+// What bounds it: the logits' bytes, once from HBM; a row or two: the chain of loads, maxima and the two small sorts.  Few rows: the
+// CTAs of a cluster share a row, and the first one joins their parts through shared memory; many: a CTA a row.
+#include "vs_operators.cuh"
+#include "vs_ptx.cuh"
+
+namespace vs {
+
+namespace {
+
+constexpr int kThreads = 512, kWarps = kThreads / 32, kTop = VS_MAX_TOP, kMaxCluster = 8;
+constexpr int kAbove = 1024, kEqual = 256;             // candidates above the bound, and equal to it, that are kept
+constexpr uint32_t kLeastNumber = 0x00800000u;         // the most negative finite logit, as ordered() has it; -inf is one less, NaN 0
+constexpr float kLog2e = 1.4426950408889634f;
+
+struct ScoreArgs {
+  const void* logits;
+  const int32_t* tokens;
+  float *logprob, *entropy, *top_logprob;
+  int32_t *rank, *top_index;
+  long long row_stride;
+  int rows, vocab, top, cluster;
+};
+
+// what is known of a stretch of a row
+struct Part {
+  float m, s, u;                       // (m = -inf: nothing but -inf so far)
+  uint32_t c;
+  __device__ __forceinline__ void join(const Part& o) {
+    const float M = fmaxf(m, o.m);
+    if (M == -INFINITY) { c += o.c; return; }
+    const float da = m - M, db = o.m - M;                              // (-inf: that side is empty)
+    const float ra = da == -INFINITY ? 0.f : exp2f(da * kLog2e), rb = db == -INFINITY ? 0.f : exp2f(db * kLog2e);
+    const float sa = da == 0.f ? s : (s + (float)c) * ra, sb = db == 0.f ? o.s : (o.s + (float)o.c) * rb;
+    const float ua = da == 0.f ? u : (ra > 0.f ? ra * (u + da * (s + (float)c)) : 0.f);
+    const float ub = db == 0.f ? o.u : (rb > 0.f ? rb * (o.u + db * (o.s + (float)o.c)) : 0.f);
+    c = (da == 0.f ? c : 0u) + (db == 0.f ? o.c : 0u);
+    s = sa + sb;
+    u = ua + ub;
+    m = M;
+  }
+  // over the lanes of every aligned group of `n` (the same in each of them: both sides' sums are the same two numbers added)
+  __device__ __forceinline__ void join_lanes(int n) {
+    for (int o = n >> 1; o > 0; o >>= 1) {
+      Part q;
+      q.m = __shfl_xor_sync(0xffffffffu, m, o);
+      q.s = __shfl_xor_sync(0xffffffffu, s, o);
+      q.u = __shfl_xor_sync(0xffffffffu, u, o);
+      q.c = __shfl_xor_sync(0xffffffffu, c, o);
+      join(q);
+    }
+  }
+};
+
+__device__ __forceinline__ uint32_t ordered(float v) {                 // ascending with v; NaN below every number, -0 = 0
+  if (v != v) return 0u;
+  const uint32_t b = __float_as_uint(v + 0.f);
+  return (b & 0x80000000u) ? ~b : (b | 0x80000000u);
+}
+// (larger logit, else lower index) as one word; 0 is nobody's
+__device__ __forceinline__ unsigned long long key_of(uint32_t o, int i) { return ((unsigned long long)o << 32) | (uint32_t)(0x7fffffff - i); }
+
+template <typename T>
+struct Vec { static constexpr int n = 16 / (int)sizeof(T); };
+
+// the logits of vector i of a row: those behind its end as -inf
+template <typename T, bool kVector>
+__device__ __forceinline__ uint4 fetch(const T* row, int i, int vocab) {
+  constexpr int V = Vec<T>::n;
+  if (kVector && (i + 1) * V <= vocab) return __ldg(reinterpret_cast<const uint4*>(row) + i);
+  uint32_t w[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    if constexpr (sizeof(T) == 4) {
+      w[j] = i * V + j < vocab ? __float_as_uint(row[i * V + j]) : 0xff800000u;
+    } else {
+      const uint16_t* r = reinterpret_cast<const uint16_t*>(row);
+      const uint32_t lo = i * V + 2 * j < vocab ? r[i * V + 2 * j] : 0xff80u, hi = i * V + 2 * j + 1 < vocab ? r[i * V + 2 * j + 1] : 0xff80u;
+      w[j] = lo | (hi << 16);
+    }
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+template <typename T>
+__device__ __forceinline__ float element(const uint4& v, int j) {
+  if constexpr (sizeof(T) == 4) return __uint_as_float(word(v, j));
+  else return (j & 1) ? __uint_as_float(word(v, j >> 1) & 0xffff0000u) : __uint_as_float(word(v, j >> 1) << 16);
+}
+
+__device__ __forceinline__ unsigned long long ld_peer_u64(uint32_t addr) {
+  unsigned long long v;
+  asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(addr) : "memory");
+  return v;
+}
+
+struct Shared {
+  unsigned long long above[kAbove], equal[kEqual + kTop], best[kMaxCluster * kTop];
+  Part part[kWarps];
+  int before[kWarps], odd[kWarps];     // logits that come before the token; whether a NaN or +inf was met
+  Part whole;                          // this CTA's part of the row, for the cluster's first
+  int n_before, n_odd, n_above, n_equal;
+  uint32_t bound;
+};
+
+template <typename T, bool kVector>
+__global__ void __launch_bounds__(kThreads, 2) token_logprobs_kernel(const __grid_constant__ ScoreArgs a) {
+  __shared__ Shared sm;
+  constexpr int V = Vec<T>::n, E = 16, U = E / V;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int C = a.cluster, row_i = (int)blockIdx.x / C, rank = (int)blockIdx.x - row_i * C;
+  const T* row = static_cast<const T*>(a.logits) + (long long)row_i * a.row_stride;
+  const int nv = (a.vocab + V - 1) / V;
+  const int v0 = (int)((long long)nv * rank / C), v1 = (int)((long long)nv * (rank + 1) / C);
+  const int token = a.tokens != nullptr ? a.tokens[row_i] : -1;
+  const bool has_token = token >= 0 && token < a.vocab;
+  const uint4 nothing = sizeof(T) == 4 ? make_uint4(0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u) : make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u);
+  uint4 next[U];
+#pragma unroll
+  for (int j = 0; j < U; ++j) next[j] = v0 + tid + j * kThreads < v1 ? fetch<T, kVector>(row, v0 + tid + j * kThreads, a.vocab) : nothing;
+  float xt = INFINITY;                 // (no token: nothing comes before it)
+  if (has_token) {
+    if constexpr (sizeof(T) == 4) xt = row[token];
+    else xt = __bfloat162float(row[token]);
+  }
+  const bool xt_nan = xt != xt;
+
+  // ---- one pass: running maximum, sums, place of the token --------------------------------------------------
+  Part p = {-INFINITY, 0.f, 0.f, 0u};
+  int n_before = 0;
+  bool odd = false;
+  for (int v = v0 + tid; v < v1; v += U * kThreads) {
+    uint4 now[U];
+#pragma unroll
+    for (int j = 0; j < U; ++j) {
+      now[j] = next[j];
+      const int w = v + (U + j) * kThreads;
+      next[j] = w < v1 ? fetch<T, kVector>(row, w, a.vocab) : nothing;
+    }
+    float x[E];
+    float most = -INFINITY;
+#pragma unroll
+    for (int j = 0; j < U; ++j)
+#pragma unroll
+      for (int e = 0; e < V; ++e) { x[j * V + e] = element<T>(now[j], e); most = fmaxf(most, x[j * V + e]); }
+    // the order: x > xt, or equal with a lower index
+#pragma unroll
+    for (int j = 0; j < U; ++j) {
+      const int i0 = (v + j * kThreads) * V;
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        const float y = x[j * V + e];
+        const bool tie = y == xt && i0 + e < token;
+        n_before += (y > xt || tie) ? 1 : 0;
+      }
+    }
+    if (xt_nan) {
+#pragma unroll
+      for (int j = 0; j < U; ++j)
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          const int i = (v + j * kThreads) * V + e;
+          n_before += (v + j * kThreads < v1 && i < a.vocab && (x[j * V + e] == x[j * V + e] || i < token)) ? 1 : 0;
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < E; ++i) odd = odd || !(x[i] <= 3.402823466e38f);      // NaN or +inf
+    if (most >= p.m) {
+      if (most > p.m) {
+        if (p.m != -INFINITY) {
+          const float d = p.m - most, r = exp2f(d * kLog2e);
+          p.u = r > 0.f ? r * (p.u + d * (p.s + (float)p.c)) : 0.f;
+          p.s = (p.s + (float)p.c) * r;
+        }
+        p.c = 0u;
+        p.m = most;
+      }
+      if (most == -INFINITY) continue;
+#pragma unroll
+      for (int i = 0; i < E; ++i) {
+        const float d = fmaxf(x[i] - p.m, -1000.f);                     // (-inf: 2^-1443 = 0, and 0 in u)
+        const float e = d < 0.f ? exp2f(d * kLog2e) : 0.f;
+        p.c += d < 0.f ? 0u : 1u;
+        p.s += e;
+        p.u = fmaf(d, e, p.u);
+      }
+    } else {
+      float s = 0.f, u = 0.f;
+#pragma unroll
+      for (int i = 0; i < E; ++i) {
+        const float d = fmaxf(x[i] - p.m, -1000.f), e = exp2f(d * kLog2e);
+        s += e;
+        u = fmaf(d, e, u);
+      }
+      p.s += s;
+      p.u += u;
+    }
+  }
+  const uint32_t own_max = ordered(p.m);
+  p.join_lanes(32);
+  n_before = __reduce_add_sync(0xffffffffu, n_before);
+  odd = __any_sync(0xffffffffu, odd);
+  if (lane == 0) { sm.part[warp] = p; sm.before[warp] = n_before; sm.odd[warp] = odd; }
+  if (tid == 0) { sm.n_above = 0; sm.n_equal = 0; }
+  __syncthreads();
+  if (warp == 0) {
+    Part w = sm.part[lane & (kWarps - 1)];
+    w.join_lanes(kWarps);
+    const int b = __reduce_add_sync(0xffffffffu, lane < kWarps ? sm.before[lane] : 0);
+    const bool o = __any_sync(0xffffffffu, lane < kWarps && sm.odd[lane & (kWarps - 1)] != 0);
+    if (lane == 0) { sm.whole = w; sm.n_before = b; sm.n_odd = o; }
+  }
+
+  // ---- the best of this CTA's part -----------------------------------------------------------------------------
+  const int k = a.top;
+  if (k > 0) {
+    // a bound that at least k of the threads' maxima reach, bit by bit from the top (the last 14 bits would sharpen it little)
+    uint32_t bound = 0u;
+    for (int bit = 31; bit >= 14; --bit) {
+      const uint32_t higher = bound | (1u << bit);
+      if (__syncthreads_count(own_max >= higher) >= k) bound = higher;
+    }
+    bound = max(bound, kLeastNumber);
+    for (;;) {
+      // a warp reads a thread's logits again, its lanes side by side
+      for (unsigned left = __ballot_sync(0xffffffffu, own_max >= bound); left != 0u; left &= left - 1u) {
+        const int t = warp * 32 + __ffs(left) - 1;
+        for (int v = v0 + t + lane * kThreads; v < v1; v += 32 * kThreads) {
+          const uint4 w = fetch<T, kVector>(row, v, a.vocab);
+#pragma unroll
+          for (int e = 0; e < V; ++e) {
+            const uint32_t o = ordered(element<T>(w, e));
+            const int i = v * V + e;
+            if (o < bound || i >= a.vocab) continue;
+            if (o > bound) { const int at = atomicAdd(&sm.n_above, 1); if (at < kAbove) sm.above[at] = key_of(o, i); }
+            else { const int at = atomicAdd(&sm.n_equal, 1); if (at < kEqual) sm.equal[at] = key_of(o, i); }
+          }
+        }
+      }
+      __syncthreads();
+      if (sm.n_above <= kAbove) break;
+      // more than are kept: the k-th of those kept is a higher bound that k logits reach
+      for (int c = tid; c < kAbove; c += kThreads) {
+        const unsigned long long mine = sm.above[c];
+        int place = 0;
+        for (int i = 0; i < kAbove; ++i) place += sm.above[i] > mine ? 1 : 0;
+        if (place == k - 1) sm.bound = (uint32_t)(mine >> 32);
+      }
+      __syncthreads();
+      bound = sm.bound;
+      if (tid == 0) { sm.n_above = 0; sm.n_equal = 0; }
+      __syncthreads();
+    }
+    const int n_above = sm.n_above, n_found = sm.n_equal;
+    int n_equal = min(n_found, kEqual);
+    if (n_above + n_equal < k || (n_found > kEqual && n_above < k)) {
+      // a great many equal to the bound, or fewer numbers than asked for (a masked vocabulary, a short part): the first ones in order of
+      // their index that equal the bound, then -inf, then NaN, by one warp
+      __syncthreads();
+      if (warp == 0) {
+        int have = n_found > kEqual ? 0 : n_equal;
+        for (int round = n_found > kEqual ? 0 : 1; round < 3; ++round) {
+          const uint32_t wanted = round == 0 ? bound : (round == 1 ? kLeastNumber - 1u : 0u);
+          for (int v = v0; v < v1 && have < k - n_above; v += 32) {
+            const uint4 w = v + lane < v1 ? fetch<T, kVector>(row, v + lane, a.vocab) : nothing;
+            uint32_t hits = 0u;
+#pragma unroll
+            for (int e = 0; e < V; ++e)
+              hits |= (v + lane < v1 && (v + lane) * V + e < a.vocab && ordered(element<T>(w, e)) == wanted) ? 1u << e : 0u;
+            int sum = __popc(hits);
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) { const int t = __shfl_up_sync(0xffffffffu, sum, o); if (lane >= o) sum += t; }
+            int at = have + sum - __popc(hits);
+#pragma unroll
+            for (int e = 0; e < V; ++e)
+              if ((hits >> e) & 1u) { if (at < k) sm.equal[at] = key_of(wanted, (v + lane) * V + e); ++at; }
+            have += __shfl_sync(0xffffffffu, sum, 31);
+          }
+        }
+        if (lane == 0) sm.n_equal = min(have, k - n_above);
+      }
+      __syncthreads();
+      n_equal = sm.n_equal;
+    }
+    const int n = n_above + (n_above < k ? n_equal : 0);
+    // in order, by counting; a part of few logits may hold fewer than k
+    if (tid >= n && tid < k) sm.best[tid] = 0ull;
+    for (int c = tid; c < n; c += kThreads) {
+      const unsigned long long mine = c < n_above ? sm.above[c] : sm.equal[c - n_above];
+      int place = 0;
+      for (int i = 0; i < n; ++i) place += (i < n_above ? sm.above[i] : sm.equal[i - n_above]) > mine ? 1 : 0;
+      if (place < k) sm.best[place] = mine;
+    }
+  }
+  __syncthreads();
+
+  // ---- the row ------------------------------------------------------------------------------------------------
+  if (C > 1) {
+    cluster_arrive_release();
+    cluster_wait_acquire();
+    if (rank == 0) {
+      if (warp == 0) {
+        if (lane < C) {
+          const uint32_t at = map_shared_rank(smem_u32(&sm.whole), (uint32_t)lane), counts = map_shared_rank(smem_u32(&sm.n_before), (uint32_t)lane);
+          const unsigned long long w0 = ld_peer_u64(at), w1 = ld_peer_u64(at + 8), w2 = ld_peer_u64(counts);
+          sm.part[lane] = {__uint_as_float((uint32_t)w0), __uint_as_float((uint32_t)(w0 >> 32)), __uint_as_float((uint32_t)w1), (uint32_t)(w1 >> 32)};
+          sm.before[lane] = (int)(uint32_t)w2;
+          sm.odd[lane] = (int)(w2 >> 32);
+        }
+      } else if (warp < C && lane < k) {
+        sm.best[warp * kTop + lane] = ld_peer_u64(map_shared_rank(smem_u32(&sm.best[lane]), (uint32_t)warp));
+      }
+      __syncthreads();
+      // every part's best are in order: a key's place is its own there and, by halving, how many of the other parts' come before it
+      const int c = tid / kTop, j = tid - c * kTop;
+      if (c < C && j < k) {
+        const unsigned long long mine = sm.best[c * kTop + j];
+        int place = j;
+        for (int q = 0; q < C; ++q) {
+          if (q == c) continue;
+          int lo = 0, hi = k;
+          while (lo < hi) { const int mid = (lo + hi) >> 1; if (sm.best[q * kTop + mid] > mine) lo = mid + 1; else hi = mid; }
+          place += lo;
+        }
+        if (mine != 0ull && place < k) sm.above[place] = mine;
+      }
+      __syncthreads();
+    }
+    cluster_arrive_release();          // (a peer's shared memory is read: it stays until then)
+    cluster_wait_acquire();
+    if (rank != 0) return;
+  }
+  if (warp != 0) return;
+  const unsigned long long* best = C > 1 ? sm.above : sm.best;
+  Part whole = sm.whole;
+  int all_before = sm.n_before;
+  bool bad = sm.n_odd != 0;
+  if (C > 1) {
+    whole = sm.part[lane & (C - 1)];
+    whole.join_lanes(C);
+    all_before = __reduce_add_sync(0xffffffffu, lane < C ? sm.before[lane] : 0);
+    bad = __any_sync(0xffffffffu, sm.odd[lane & (C - 1)] != 0);
+  }
+  const float nan = __int_as_float(0x7fc00000);
+  const float log_sum = logf((float)whole.c) + log1pf(whole.s / (float)whole.c);          // of e^{x - m}
+  const bool empty = whole.m == -INFINITY;                              // nothing but -inf (and NaN)
+  auto logprob_of = [&](float x) { return bad ? nan : (empty ? -INFINITY : (x - whole.m) - log_sum); };
+  if (tid == 0) {
+    if (a.logprob != nullptr) a.logprob[row_i] = has_token ? logprob_of(xt) : (token < 0 ? 0.f : nan);
+    if (a.rank != nullptr) a.rank[row_i] = has_token ? all_before : -1;
+    if (a.entropy != nullptr) a.entropy[row_i] = bad ? nan : (empty ? 0.f : fmaxf(log_sum - whole.u / (whole.s + (float)whole.c), 0.f));
+  }
+  if (tid < k) {
+    const int i = 0x7fffffff - (int)(uint32_t)best[tid];
+    if (a.top_index != nullptr) a.top_index[(long long)row_i * k + tid] = i;
+    if (a.top_logprob != nullptr) {
+      float x;
+      if constexpr (sizeof(T) == 4) x = row[i];
+      else x = __bfloat162float(row[i]);
+      a.top_logprob[(long long)row_i * k + tid] = logprob_of(x);
+    }
+  }
+}
+
+template <typename T, bool kVector>
+int launch(const ScoreArgs& a, cudaStream_t st) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(a.rows * a.cluster));
+  cfg.blockDim = dim3(kThreads);
+  cfg.stream = st;
+  cudaLaunchAttribute at = {};
+  at.id = cudaLaunchAttributeClusterDimension;
+  at.val.clusterDim.x = (unsigned)a.cluster; at.val.clusterDim.y = 1; at.val.clusterDim.z = 1;
+  cfg.attrs = &at;
+  cfg.numAttrs = a.cluster > 1 ? 1 : 0;
+  return cudaLaunchKernelEx(&cfg, token_logprobs_kernel<T, kVector>, a) == cudaSuccess ? launched() : VS_ERR_CUDA;
+}
+
+}  // namespace
+
+}  // namespace vs
+
+extern "C" int vs_token_logprobs(const void* logits, int64_t row_stride, int32_t dtype, int32_t rows, int32_t vocab, const int32_t* tokens,
+                                 int32_t top, float* logprob, float* entropy, int32_t* rank, int32_t* top_index, float* top_logprob,
+                                 int32_t device, void* cuda_stream) {
+  using namespace vs;
+  if (rows < 0 || vocab < 1 || dtype < 0 || dtype > 1 || top < 0) return VS_ERR_INVALID_ARG;
+  if (vocab > (1 << 30) || rows > (1 << 27)) return VS_ERR_UNSUPPORTED;
+  if (top > VS_MAX_TOP) return VS_ERR_CAPACITY;
+  if (top > vocab || (top > 0 && top_index == nullptr)) return VS_ERR_INVALID_ARG;
+  if ((logprob != nullptr || rank != nullptr) && rows > 0 && tokens == nullptr) return VS_ERR_INVALID_ARG;
+  if (rows == 0) return VS_OK;
+  const size_t el = dtype == 1 ? 4 : 2;
+  if (logits == nullptr || !aligned(logits, el) || !aligned(tokens, 4) || !aligned(logprob, 4) || !aligned(entropy, 4) || !aligned(rank, 4) ||
+      !aligned(top_index, 4) || !aligned(top_logprob, 4))
+    return VS_ERR_INVALID_ARG;
+  OnDevice on(device);
+  if (!on.ok) return VS_ERR_CUDA;
+  ScoreArgs a = {logits, tokens, logprob, entropy, top_logprob, rank, top_index, row_stride, rows, vocab, top, 1};
+  // CTAs of a row: as many as leave none of the first 296 places (two an SM) waiting, no more than give a thread something to read
+  const int vectors = (int)((vocab + 16 / el - 1) / (16 / el));
+  while (a.cluster < kMaxCluster && 2 * a.cluster * rows <= 296 && vectors > 2 * a.cluster * kThreads) a.cluster *= 2;
+  const bool vector = aligned(logits, 16) && (row_stride * (int64_t)el) % 16 == 0;
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  if (dtype == 1) return vector ? launch<float, true>(a, st) : launch<float, false>(a, st);
+  return vector ? launch<bf16, true>(a, st) : launch<bf16, false>(a, st);
+}

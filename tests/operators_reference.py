@@ -1,0 +1,162 @@
+"""The stand-alone operators from their definitions in 64 bits, on the CPU, one small step at a time; and how far a kernel may be off."""
+import math
+
+import torch
+
+PAGE = 64
+E_MIN, E_MAX = -110, 120
+HALF_STEP = {torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11, torch.float32: 2.0 ** -24}
+
+
+def axes_of_pairs(sections, interleaved):
+    left, out = list(sections), []
+    while sum(left):
+        for a in range(len(left)):
+            while left[a]:
+                out.append(a)
+                left[a] -= 1
+                if interleaved:
+                    break
+    return out
+
+
+def rope(x, positions, sections, theta, interleaved, inverse):
+    """-> (y, bound on |error| of fp32 arithmetic before the final rounding)."""
+    x = x.double().cpu()
+    half = x.shape[-1] // 2
+    axes = axes_of_pairs(sections, interleaved)
+    y = torch.empty_like(x)
+    bound = torch.empty_like(x)
+    for k in range(half):
+        t = positions[axes[k]].cpu().double() * theta ** (-k / half) * (-1 if inverse else 1)
+        c, s = torch.cos(t)[:, None], torch.sin(t)[:, None]
+        y[..., k] = x[..., k] * c - x[..., k + half] * s
+        y[..., k + half] = x[..., k + half] * c + x[..., k] * s
+        # a fraction of a turn rounded to fp32 (2^-25 of a turn at most), its sine and cosine to 2 units, two products and a sum; the angle
+        # itself in fp64, here and there (2^-50 of the angle)
+        off = 2 * math.pi * 2.0 ** -25 + 2 * 2.0 ** -23 + 3 * 2.0 ** -24 + 2.0 ** -50 * t.abs()[:, None]
+        bound[..., k] = bound[..., k + half] = (x[..., k].abs() + x[..., k + half].abs()) * off
+    return y, bound
+
+
+def nearest_code(y):
+    """The nearest e4m3 value, ties to even, magnitudes above 448 to 448."""
+    e = torch.floor(torch.log2(y.abs().clamp(min=2.0 ** -6, max=2.0 ** 100)))
+    step = torch.exp2(e - 3)
+    return (torch.round(y / step) * step).clamp(-448, 448)
+
+
+class Cache:
+    """Values of the codes and scales of a paged cache, as fp64 on the CPU."""
+
+    def __init__(self, k, v, k_scale, v_scale):
+        self.codes = [t.cpu().float().double() for t in (k, v)]
+        self.scale = [t.cpu().double() for t in (k_scale, v_scale)]
+
+    def pages(self, table, i, t):
+        page = int(table[i][t // PAGE]) if t // PAGE < len(table[i]) else -1
+        return page if 0 <= page < self.codes[0].shape[0] else -1
+
+    def write(self, table, start, lens, k, v):
+        for which, rows in enumerate((k, v)):
+            rows = rows.cpu().double()
+            r = 0
+            for i, n in enumerate(lens):
+                t, end = start[i], start[i] + n
+                while t < end:
+                    m = min(PAGE - t % PAGE, end - t)
+                    page = self.pages(table, i, t)
+                    if page >= 0:
+                        self._write(which, page, t % PAGE, rows[r:r + m])
+                    t += m
+                    r += m
+
+    def _write(self, which, page, at, rows):
+        codes, scale = self.codes[which], self.scale[which]
+        for h in range(rows.shape[1]):
+            x = rows[:, h]
+            fine = x[torch.isfinite(x)].abs()
+            amax = float(fine.max()) if fine.numel() else 0.0
+            e = E_MIN
+            while e < E_MAX and amax > 448 * 2.0 ** e:
+                e += 1
+            if at:
+                old = float(scale[page, h])
+                e_old = min(max(math.frexp(old)[1] - 1 if old > 0 else E_MIN, E_MIN), E_MAX)
+                if e > e_old:
+                    codes[page, h, :at] = nearest_code(codes[page, h, :at] * 2.0 ** (e_old - e))
+                e = max(e, e_old)
+            codes[page, h, at:at + len(x)] = nearest_code(x * 2.0 ** -e)
+            scale[page, h] = 2.0 ** e
+
+    def rows(self, which, table, i, t0, t1):
+        """[t1 - t0, Hkv, D] values, and which of the tokens there are."""
+        hkv, _, d = self.codes[0].shape[1:]
+        out, there = torch.zeros((t1 - t0, hkv, d), dtype=torch.float64), torch.zeros(t1 - t0, dtype=torch.bool)
+        for t in range(t0, t1):
+            page = self.pages(table, i, t)
+            if page >= 0:
+                out[t - t0] = self.codes[which][page, :, t % PAGE] * self.scale[which][page][:, None]
+                there[t - t0] = True
+        return out, there
+
+    def attend(self, table, lengths, lens, q, scale, causal=True, window=0):
+        """-> (out, lse, bound on |error| of the rows before their rounding, bound of lse)."""
+        q = q.cpu().double()
+        hkv, d = self.codes[0].shape[1], self.codes[0].shape[3]
+        group = q.shape[1] // hkv
+        out, off = torch.zeros_like(q), torch.zeros_like(q)
+        lse, lse_off = torch.full(q.shape[:2], -math.inf, dtype=torch.float64), torch.zeros(q.shape[:2], dtype=torch.float64)
+        r = 0
+        for i, n in enumerate(lens):
+            total = max(int(lengths[i]), 0)
+            k, there = self.rows(0, table, i, 0, total)
+            v, _ = self.rows(1, table, i, 0, total)
+            for t in range(n):
+                pos = total - n + t
+                j = torch.arange(total)
+                seen = there.clone()
+                if causal:
+                    seen &= j <= pos
+                if window:
+                    seen &= j > pos - window
+                for h in range(q.shape[1]):
+                    if not bool(seen.any()):
+                        continue
+                    kk, vv = k[seen, h // group], v[seen, h // group]
+                    s = kk @ q[r, h] * scale
+                    p = torch.softmax(s, 0)
+                    out[r, h] = p @ vv
+                    lse[r, h] = torch.logsumexp(s, 0)
+                    # scores: d products summed in fp32, a factor of two roundings, the running maximum's and the exponent's few; weights
+                    # to 11 bits and 2^x to 2 units; sums of all keys
+                    size = float((kk.abs() @ q[r, h].abs()).max()) * scale
+                    ds = (d + 4) * 2.0 ** -24 * size + 6 * 2.0 ** -24 * (float(s.abs().max()) + 256)
+                    dw = 2 * ds + 2.0 ** -11 + (len(s) + 64) * 2.0 ** -24
+                    off[r, h] = 2 * dw * (p @ vv.abs()) + 2.0 ** -38 * vv.abs().amax(0) * len(s)
+                    lse_off[r, h] = dw - 2.0 ** -11 + 2.0 ** -22 * abs(float(lse[r, h]))
+                r += 1
+        return out, lse, off, lse_off
+
+
+def token_logprobs(logits, tokens, top):
+    """Lists by row: (logprob, entropy, rank, [index], [logprob of it])."""
+    got = []
+    for row, t in zip(logits.cpu().double(), tokens.cpu().tolist()):
+        x = row.tolist()
+        key = lambda i: (x[i] != x[i], -x[i] if x[i] == x[i] else 0.0, i)
+        order = sorted(range(len(x)), key=key)
+        bad = any(v != v or v == math.inf for v in x)
+        empty = all(v == -math.inf for v in x)
+        if bad or empty:
+            lp = lambda i: math.nan if bad else -math.inf
+            entropy = math.nan if bad else 0.0
+        else:
+            m = max(x)
+            rest = math.fsum(math.exp(v - m) for v in x) - 1.0 if len(x) > 1 else 0.0
+            lse = m + math.log1p(rest)
+            lp = lambda i: x[i] - lse
+            entropy = math.fsum(-math.exp(v - lse) * (v - lse) for v in x if v > -math.inf)
+        got.append((0.0 if t < 0 else (math.nan if t >= len(x) else lp(t)), entropy, order.index(t) if 0 <= t < len(x) else -1,
+                    order[:top], [lp(i) for i in order[:top]]))
+    return got
