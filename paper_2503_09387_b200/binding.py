@@ -441,7 +441,14 @@ class PageCache:
         import torch
         out = C.c_size_t(0)
         _check(load_library().vs_cache_attention_bytes(self.head_dim, C.byref(out)), "vs_cache_attention_bytes")
-        return torch.empty(out.value, dtype=torch.uint8, device=self.k.device)
+        workspace = torch.empty(out.value, dtype=torch.uint8, device=self.k.device)
+        workspace[:256].zero_()
+        return workspace
+
+    def attend_status(self) -> int:
+        """0, or VS_ERR_DEVICE_TIMEOUT if a wait of an ``attend`` with one of the cache's own workspaces ever ran out.  Synchronises."""
+        import torch
+        return min([int(w[:4].view(torch.int32).item()) for w in self._workspaces.values()], default=VS_OK)
 
     def attend(self, page_table, lengths, q, out=None, lse=None, row_offsets=None, scale=None, causal=True, window=0, workspace=None,
                out_dtype=None):

@@ -207,36 +207,51 @@ __global__ void __launch_bounds__(kThreads) cache_attention_few_kernel(const __g
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           x[j] = fmaf(sc[n][j], factor[n][j & 1] * scales.x, evf);
-          x[j] = x[j] == x[j] ? x[j] : INFINITY;                       // (NaN goes on as infinity - infinity)
           const int key = key0 + g + 8 * (j >> 1);
           if (edge && (key >= hi_of[n][j & 1] || key < lo_of[n][j & 1])) x[j] = -INFINITY;
           mx[j & 1] = fmaxf(mx[j & 1], x[j]);
         }
-        bool moved = false;
-        float r[2];
+        bool moved = false, far[2];
+        float m_new[2];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
           mx[j] = fmaxf(mx[j], __shfl_xor_sync(0xffffffffu, mx[j], 4));
           mx[j] = fmaxf(mx[j], __shfl_xor_sync(0xffffffffu, mx[j], 8));
           mx[j] = fmaxf(mx[j], __shfl_xor_sync(0xffffffffu, mx[j], 16));
-          const float m = fmaxf(m_run[n][j], mx[j]);
-          moved = moved || m > m_run[n][j];
-          r[j] = m == -INFINITY ? 1.f : exp2f(m_run[n][j] - m);
-          m_run[n][j] = m;
+          m_new[j] = fmaxf(m_run[n][j], mx[j]);
+          moved = moved || m_new[j] > m_run[n][j];
+          far[j] = mx[j] < m_new[j] - kFar && mx[j] > -INFINITY;
         }
         if (__any_sync(0xffffffffu, moved)) {
+          float r[2];
 #pragma unroll
-          for (int j = 0; j < 2; ++j) l_run[n][j] *= r[j];
+          for (int j = 0; j < 2; ++j) {
+            const float d = m_run[n][j] - m_new[j];
+            r[j] = m_run[n][j] == -INFINITY ? 1.f : ex2_approx(d);
+            l_run[n][j] = m_run[n][j] == -INFINITY ? l_run[n][j] : times_power(l_run[n][j], d);
+            m_run[n][j] = m_new[j];
+          }
 #pragma unroll
           for (int i2 = 0; i2 < KS; ++i2)
 #pragma unroll
             for (int j = 0; j < 4; ++j) o[n][i2][j] *= r[j & 1];
         }
         float p[4];
+        if (!__any_sync(0xffffffffu, far[0] || far[1])) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          p[j] = exp2f(x[j] - (m_run[n][j & 1] == -INFINITY ? 0.f : m_run[n][j & 1] - kLift));
-          l_run[n][j & 1] = fmaf(p[j], down, l_run[n][j & 1]);
+          for (int j = 0; j < 4; ++j) {
+            p[j] = ex2_approx(x[j] - (m_run[n][j & 1] == -INFINITY ? 0.f : m_run[n][j & 1] - kLift));
+            l_run[n][j & 1] = fmaf(p[j], down, l_run[n][j & 1]);
+          }
+        } else {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int c = j & 1;
+            const float ref = far[c] ? mx[c] : (m_run[n][c] == -INFINITY ? 0.f : m_run[n][c] - kLift);
+            p[j] = ex2_approx(x[j] - ref);
+            l_run[n][c] = fmaf(p[j], far[c] ? exp2f(mx[c] - m_run[n][c] + kLift - evf) : down, l_run[n][c]);
+            if (far[c]) p[j] = 0.f;
+          }
         }
         pf[n][0] = transpose_8x8(half2_of(p[0], p[1]));
         pf[n][1] = transpose_8x8(half2_of(p[2], p[3]));
@@ -284,7 +299,7 @@ __global__ void __launch_bounds__(kThreads) cache_attention_few_kernel(const __g
         l += __shfl_xor_sync(0xffffffffu, l, 8);
         l += __shfl_xor_sync(0xffffffffu, l, 16);
         const int col = 8 * n + 2 * q4 + j;
-        if (g == 0) stats[warp * W + col] = make_float2(m_run[n][j], l);
+        if (g == 0) stats[warp * W + col] = make_float2(l == l ? m_run[n][j] : INFINITY, l);      // (NaN goes on as infinity - infinity)
         float* row = rows + (warp * W + col) * F::kRowF + (D / 8) * g;
 #pragma unroll
         for (int i = 0; i < KS; ++i) { row[2 * i] = o[n][i][j]; row[2 * i + 1] = o[n][i][j + 2]; }
@@ -306,7 +321,7 @@ __global__ void __launch_bounds__(kThreads) cache_attention_few_kernel(const __g
         const float f = st.x == -INFINITY ? 0.f : exp2f(st.x - m);
         const float4 x = *reinterpret_cast<const float4*>(rows + (w * W + col) * F::kRowF + d);
         v.x = fmaf(f, x.x, v.x); v.y = fmaf(f, x.y, v.y); v.z = fmaf(f, x.z, v.z); v.w = fmaf(f, x.w, v.w);
-        l = fmaf(f, st.y, l);
+        l += st.x == -INFINITY ? 0.f : times_power(st.y, st.x - m);
       }
       if (part != nullptr) {
         *reinterpret_cast<float4*>(part + (size_t)col * D + d) = v;
@@ -325,62 +340,90 @@ __global__ void __launch_bounds__(kThreads) cache_attention_few_kernel(const __g
 }
 
 // ---- rows that several CTAs worked on ------------------------------------------------------------------------------
-// A block a (CTA that was the last on its item, column): eight warps take the parts by turns, a lane four dims.
-constexpr int kJoinWarps = 8;
-template <int W, int D>
-__global__ void __launch_bounds__(32 * kJoinWarps) cache_attention_join_kernel(const __grid_constant__ CacheAttnArgs a) {
-  __shared__ float sm_m[kJoinWarps], sm_l[kJoinWarps];
-  __shared__ float4 sm_o[kJoinWarps][D / 4];
+// A block lists the CTAs that were the last on an item others had begun, then takes columns of those items by turns: kCols at a time, the
+// parts of each shared by 8 / kCols warps, a lane four dims.
+constexpr int kJoinThreads = 256, kJoinBlocks = 4 * 148;
+template <int W, int D, int kCols>
+__global__ void __launch_bounds__(kJoinThreads) cache_attention_join_kernel(const __grid_constant__ CacheAttnArgs a, int ctas) {
+  constexpr int WPC = 8 / kCols, GROUPS = W / kCols, U = 4;
+  constexpr int CHUNKS = (kFewCtas + 31) / 32;
+  __shared__ int list[kFewCtas], count[CHUNKS];
+  __shared__ float2 sm_st[8];
+  __shared__ float4 sm_o[8][D / 4];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   pdl_wait();
-  const int last = (int)blockIdx.x, col = (int)blockIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int4 j = a.joins[last];
-  if (j.x == 0 || col >= (j.w >> 16)) return;
-  const int first = j.x - 1;
-  float m = -INFINITY, l = 0.f;
-  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-  constexpr int U = 4;
-  for (int c0 = first + warp; c0 <= last; c0 += U * kJoinWarps) {
-    float2 st[U];
-    float4 v[U];
+  // (in the order of the CTAs: the same list in every block)
+  unsigned set[(CHUNKS + 7) / 8];
 #pragma unroll
-    for (int i = 0; i < U; ++i) {
-      const int c = c0 + i * kJoinWarps;
-      st[i] = make_float2(-INFINITY, 0.f);
-      v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (c <= last) {
-        const int place = c == first ? 1 : 0;
-        st[i] = part_stats<W, D>(a.parts, c, place)[col];
-        if (lane < D / 4) v[i] = *reinterpret_cast<const float4*>(part_rows<W, D>(a.parts, c, place) + (size_t)col * D + 4 * lane);
+  for (int k = 0; k < (CHUNKS + 7) / 8; ++k) {
+    const int chunk = warp + 8 * k, c = 32 * chunk + lane;
+    set[k] = __ballot_sync(0xffffffffu, c < ctas && a.joins[min(c, ctas - 1)].x != 0);
+    if (lane == 0 && chunk < CHUNKS) count[chunk] = __popc(set[k]);
+  }
+  __syncthreads();
+  int listed = 0;
+  for (int i = 0; i < CHUNKS; ++i) listed += count[i];
+#pragma unroll
+  for (int k = 0; k < (CHUNKS + 7) / 8; ++k) {
+    const int chunk = warp + 8 * k;
+    int at = __popc(set[k] & ((1u << lane) - 1u));
+    for (int i = 0; i < min(chunk, CHUNKS); ++i) at += count[i];
+    if ((set[k] >> lane) & 1u) list[at] = 32 * chunk + lane;
+  }
+  __syncthreads();
+  const int n = listed * GROUPS;
+  for (int at = (int)blockIdx.x; at < n; at += (int)gridDim.x) {
+    const int last = list[at / GROUPS], col = (at % GROUPS) * kCols + warp / WPC, share = warp % WPC;
+    const int4 j = a.joins[last];
+    const int first = j.x - 1;
+    const bool on = col < (j.w >> 16);
+    float m = -INFINITY, l = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int c0 = first + share; c0 <= last && on; c0 += U * WPC) {
+      float2 st[U];
+      float4 v[U];
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        const int c = c0 + i * WPC;
+        st[i] = make_float2(-INFINITY, 0.f);
+        v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (c <= last) {
+          const int place = c == first ? 1 : 0;
+          st[i] = part_stats<W, D>(a.parts, c, place)[col];
+          if (lane < D / 4) v[i] = *reinterpret_cast<const float4*>(part_rows<W, D>(a.parts, c, place) + (size_t)col * D + 4 * lane);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        if (st[i].x == -INFINITY) continue;
+        const float m_new = fmaxf(m, st[i].x), fa = m == -INFINITY ? 0.f : exp2f(m - m_new), fb = exp2f(st[i].x - m_new);
+        o.x = o.x * fa + v[i].x * fb; o.y = o.y * fa + v[i].y * fb; o.z = o.z * fa + v[i].z * fb; o.w = o.w * fa + v[i].w * fb;
+        l = (m == -INFINITY ? 0.f : times_power(l, m - m_new)) + times_power(st[i].y, st[i].x - m_new);
+        m = m_new;
       }
     }
+    if (lane == 0) sm_st[warp] = make_float2(m, l);
+    if (lane < D / 4) sm_o[warp][lane] = o;
+    __syncthreads();
+    if (on && share == 0 && lane < D / 4) {
+      float M = -INFINITY, sum = 0.f;
 #pragma unroll
-    for (int i = 0; i < U; ++i) {
-      if (st[i].x == -INFINITY) continue;
-      const float m_new = fmaxf(m, st[i].x), fa = m == -INFINITY ? 0.f : exp2f(m - m_new), fb = exp2f(st[i].x - m_new);
-      o.x = o.x * fa + v[i].x * fb; o.y = o.y * fa + v[i].y * fb; o.z = o.z * fa + v[i].z * fb; o.w = o.w * fa + v[i].w * fb;
-      l = l * fa + st[i].y * fb;
-      m = m_new;
+      for (int w = 0; w < WPC; ++w) M = fmaxf(M, sm_st[warp + w].x);
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int w = 0; w < WPC; ++w) {
+        const float2 st = sm_st[warp + w];
+        const float f = st.x == -INFINITY ? 0.f : exp2f(st.x - M);
+        const float4 x = sm_o[warp + w][lane];
+        v.x += f * x.x; v.y += f * x.y; v.z += f * x.z; v.w += f * x.w;
+        sum += st.x == -INFINITY ? 0.f : times_power(st.y, st.x - M);
+      }
+      const float inv = sum == 0.f ? 0.f : 1.f / sum;
+      store_row_piece(a, j.y, j.z + col, j.w & 0xffff, 4 * lane, make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv));
+      if (lane == 0) store_lse(a, j.y, j.z + col, j.w & 0xffff, M, sum);
     }
+    __syncthreads();
   }
-  if (lane == 0) { sm_m[warp] = m; sm_l[warp] = l; }
-  if (lane < D / 4) sm_o[warp][lane] = o;
-  __syncthreads();
-  if (warp != 0 || lane >= D / 4) return;
-  float M = -INFINITY;
-#pragma unroll
-  for (int w = 0; w < kJoinWarps; ++w) M = fmaxf(M, sm_m[w]);
-  float L = 0.f;
-  float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-  for (int w = 0; w < kJoinWarps; ++w) {
-    const float f = sm_m[w] == -INFINITY ? 0.f : exp2f(sm_m[w] - M);
-    const float4 x = sm_o[w][lane];
-    v.x += f * x.x; v.y += f * x.y; v.z += f * x.z; v.w += f * x.w;
-    L += f * sm_l[w];
-  }
-  const float inv = L == 0.f ? 0.f : 1.f / L;
-  store_row_piece(a, j.y, j.z + col, j.w & 0xffff, 4 * lane, make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv));
-  if (lane == 0) store_lse(a, j.y, j.z + col, j.w & 0xffff, M, L);
 }
 
 template <int D, int NT>
@@ -392,18 +435,18 @@ int launch_few(const CacheAttnArgs& a, int ctas, cudaStream_t st) {
   return launched();
 }
 
-template <int W, int D>
+template <int W, int D, int kCols>
 int launch_join(const CacheAttnArgs& a, int ctas, cudaStream_t st) {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)ctas, (unsigned)W);
-  cfg.blockDim = dim3(32 * kJoinWarps);
+  cfg.gridDim = dim3(kJoinBlocks);
+  cfg.blockDim = dim3(kJoinThreads);
   cfg.stream = st;
   cudaLaunchAttribute at = {};
   at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
   at.val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = &at;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, cache_attention_join_kernel<W, D>, a) == cudaSuccess ? launched() : VS_ERR_CUDA;
+  return cudaLaunchKernelEx(&cfg, cache_attention_join_kernel<W, D, kCols>, a, ctas) == cudaSuccess ? launched() : VS_ERR_CUDA;
 }
 
 }  // namespace
@@ -413,21 +456,25 @@ int launch_cache_attention_few(const CacheAttnArgs& a, int cols, int ctas, cudaS
   return a.c.head_dim == 128 ? launch_few<128, 2>(a, ctas, st) : launch_few<64, 2>(a, ctas, st);
 }
 int launch_cache_attention_join(const CacheAttnArgs& a, int width, int ctas, cudaStream_t st) {
-  if (width == 8) return a.c.head_dim == 128 ? launch_join<8, 128>(a, ctas, st) : launch_join<8, 64>(a, ctas, st);
-  return a.c.head_dim == 128 ? launch_join<16, 128>(a, ctas, st) : launch_join<16, 64>(a, ctas, st);
+  if (width == 8) return a.c.head_dim == 128 ? launch_join<8, 128, 1>(a, ctas, st) : launch_join<8, 64, 1>(a, ctas, st);
+  if (width == 16) return a.c.head_dim == 128 ? launch_join<16, 128, 1>(a, ctas, st) : launch_join<16, 64, 1>(a, ctas, st);
+  return a.c.head_dim == 128 ? launch_join<kManyWide, 128, 4>(a, ctas, st) : launch_join<kManyWide, 64, 4>(a, ctas, st);
 }
 
 }  // namespace vs
 
 namespace {
-constexpr int kFewCtas = 3 * 148, kFewMinPages = 4;
-constexpr size_t kJoinBytes = 16384;
+constexpr int kFewMinPages = 4, kManyMinPages = 6;
+// the workspace: status word, the CTAs' notes, their parts
+constexpr size_t kJoinsAt = 256, kPartsAt = 8192;
+static_assert(kJoinsAt + vs::kFewCtas * 16 <= kPartsAt && vs::kManyCtas <= vs::kFewCtas, "notes of the CTAs");
 }
 
 extern "C" int vs_cache_attention_bytes(int32_t head_dim, size_t* out_bytes) {
   if (out_bytes == nullptr) return VS_ERR_INVALID_ARG;
   if (head_dim != 64 && head_dim != 128) return VS_ERR_UNSUPPORTED;
-  *out_bytes = kJoinBytes + (size_t)kFewCtas * 2 * 16 * (head_dim + 2) * 4;
+  const size_t row = (size_t)(head_dim + 2) * 4, few = (size_t)vs::kFewCtas * 2 * vs::kFewCols * row, many = (size_t)vs::kManyCtas * 2 * vs::kManyWide * row;
+  *out_bytes = kPartsAt + (few > many ? few : many);
   return VS_OK;
 }
 
@@ -454,17 +501,31 @@ extern "C" int vs_cache_attention(const vs_cache* cache, const vs_cache_rows* ro
   CacheAttnArgs a = {};
   a.c = *cache; a.r = *rows;
   a.q = static_cast<const bf16*>(q); a.out = out; a.lse = lse;
-  a.joins = static_cast<int4*>(workspace);
-  a.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + kJoinBytes);
+  a.status = static_cast<int*>(workspace);
+  a.joins = reinterpret_cast<int4*>(static_cast<uint8_t*>(workspace) + kJoinsAt);
+  a.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + kPartsAt);
   a.q_row = q_row_stride; a.q_head = q_head_stride; a.out_row = out_row_stride; a.out_head = out_head_stride;
   a.scale_log2e = scale * 1.4426950408889634f;
   a.Hq = n_q_heads; a.G = G; a.causal = causal != 0; a.window = window; a.out_fp32 = out_dtype;
-  a.min_pages = kFewMinPages;
-  a.few_cols = 0x7fffffff; a.take_few = 1;
-  const long long most = rows->row_offsets == nullptr ? (long long)(rows->n_rows / rows->n_seqs) * G : (long long)rows->n_rows * G;
-  const int cols = most <= 8 ? 8 : 16;
+  // Which sequences have few rows the device knows; the host, from the number of rows, that all of them have (or none, where they have the
+  // same number each).
+  const bool uniform = rows->row_offsets == nullptr;
+  const long long most = (uniform ? (long long)(rows->n_rows / rows->n_seqs) : (long long)rows->n_rows) * G;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  const int r1 = launch_cache_attention_few(a, cols, kFewCtas, st);
-  if (r1 != VS_OK) return r1;
-  return launch_cache_attention_join(a, cols, kFewCtas, st);
+  if (most <= kFewCols || !uniform) {
+    a.take_few = 1;
+    a.min_pages = kFewMinPages;
+    const int cols = most <= 8 ? 8 : 16;
+    int r = launch_cache_attention_few(a, cols, kFewCtas, st);
+    if (r == VS_OK) r = launch_cache_attention_join(a, cols, kFewCtas, st);
+    if (r != VS_OK) return r;
+  }
+  if (most > kFewCols) {
+    a.take_few = 0;
+    a.min_pages = kManyMinPages;
+    int r = launch_cache_attention_many(a, kManyCtas, st);
+    if (r == VS_OK) r = launch_cache_attention_join(a, kManyWide, kManyCtas, st);
+    if (r != VS_OK) return r;
+  }
+  return VS_OK;
 }

@@ -4,6 +4,9 @@
 
 namespace vs {
 
+constexpr int kFewCols = 16;      // sequences of at most as many packed rows: vs_cache_attention.cu; more: vs_cache_attention_tc.cu
+constexpr int kFewCtas = 3 * 148, kManyCtas = 148, kManyWide = 256;
+
 struct CacheAttnArgs {
   vs_cache c;
   vs_cache_rows r;
@@ -11,12 +14,13 @@ struct CacheAttnArgs {
   void* out;
   float* lse;                     // [n_rows][Hq], or null
   float* parts;                   // workspace: unnormalised rows of items that several CTAs share
-  int4* joins;                    // ... and, per CTA, which item it was the last to work on: see AttnJoin
+  int4* joins;                    // ... and, per CTA, which item it was the last to work on
+  int* status;                    // VS_ERR_DEVICE_TIMEOUT if a wait ran out
   long long q_row, q_head, out_row, out_head;
   float scale_log2e;
   int Hq, G, causal, window, out_fp32;
   int min_pages;                  // pages that are worth a CTA of their own
-  int few_cols, take_few;         // sequences of at most few_cols rows times heads of a group go to one kernel, the others to the other
+  int take_few;                   // whether the launch takes the sequences of few rows or the others
 };
 
 #ifdef __CUDACC__
@@ -28,7 +32,7 @@ __device__ __forceinline__ SeqShape shape_of(const CacheAttnArgs& a, int i) {
   const SeqRows s = rows_of(a.r, i);
   SeqShape q = {s.first, s.n, max(a.r.tokens[i], 0), 0};
   const long long cols = (long long)s.n * a.G;
-  if ((cols <= a.few_cols) == (a.take_few != 0)) q.tiles = (int)((cols + W - 1) / W);
+  if ((cols <= kFewCols) == (a.take_few != 0)) q.tiles = (int)((cols + W - 1) / W);
   return q;
 }
 // keys [lo, hi) that row t of a sequence sees
@@ -124,6 +128,14 @@ __device__ __forceinline__ int cta_of(long long units, int ctas, long long unit)
   return c;
 }
 
+// A row's sum l goes by the scores alone and its reference m by score and page exponent: with pages whose exponents lie 230 apart 2^d, d <= 0, may
+// be nothing where l 2^d is not.  In two halves.
+__device__ __forceinline__ float times_power(float l, float d) {
+  const float h = exp2f(0.5f * d);
+  return l * h * h;
+}
+constexpr float kFar = 40.f;      // a page whose largest x lies as far below m adds nothing to a row's O; to its l perhaps
+
 // where packed row r (of a sequence whose rows begin at `first`) of KV head h is stored
 __device__ __forceinline__ void store_row_piece(const CacheAttnArgs& a, int first, int r, int head, int d, float4 v) {
   const int t = r / a.G, g = r - t * a.G;
@@ -142,6 +154,7 @@ __device__ __forceinline__ void store_lse(const CacheAttnArgs& a, int first, int
 #endif
 
 int launch_cache_attention_few(const CacheAttnArgs& a, int cols, int ctas, cudaStream_t st);
+int launch_cache_attention_many(const CacheAttnArgs& a, int ctas, cudaStream_t st);
 int launch_cache_attention_join(const CacheAttnArgs& a, int width, int ctas, cudaStream_t st);
 
 }  // namespace vs

@@ -269,6 +269,7 @@ def attend_case(hkv, group, d, lengths, lens, seed=0, causal=True, window=0, out
     o, l, o_off, l_off = want.attend(table.tolist(), lengths, lens, q, scale, causal, window)
     close(out, o, o_off, "rows")
     close(lse, l, l_off, "lse")
+    assert cache.attend_status() == 0
     assert bool((guard[0] == 77).all()) and bool((guard[-1] == 77).all())
     return cache, table, q, out, lse
 
