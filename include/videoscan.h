@@ -305,7 +305,7 @@ int vs_destroy_stream(vs_stream* h);
  *   (y_k, y_{k + D/2}) = (x_k cos t - x_{k + D/2} sin t,  x_{k + D/2} cos t + x_k sin t),
  *   t = positions[axis(k)][row] * theta^(-2k / D);
  * inverse != 0 turns back by the same angle (which is also the gradient with respect to x).
- * sections: HOST [n_axes], pairs of each axis (may be 0), their sum D/2.  interleaved = 0: the axes'
+ * sections: pairs of each axis (may be 0), their sum D/2.  interleaved = 0: the axes'
  * pairs one axis after the other; 1: the pairs dealt to the axes in turn, an axis that has its share
  * left out of the later rounds.  One axis: the rotation that vs_frame_prefill applies.
  * x, out: DEVICE [rows][heads][head_dim] of dtype, 16-byte aligned, strides multiples of 16 bytes,
@@ -313,11 +313,16 @@ int vs_destroy_stream(vs_stream* h);
  * positions: DEVICE int64 [n_axes][rows], pos_stride between axes; |position| < 2^31 keeps the angle
  *   exact to 1e-6.
  * head_dim: a multiple of 16 up to 256.  n_axes: 1 .. VS_MAX_AXES. */
-int vs_rope_axes(const void* x, int64_t x_row_stride, int64_t x_head_stride,
-                 void* out, int64_t out_row_stride, int64_t out_head_stride, int32_t dtype,
-                 int32_t rows, int32_t heads, int32_t head_dim,
-                 const int64_t* positions, int64_t pos_stride, int32_t n_axes, const int32_t* sections,
-                 int32_t interleaved, int32_t inverse, double theta, int32_t device, void* cuda_stream);
+typedef struct {
+  const void* x;
+  void* out;
+  const int64_t* positions;
+  int64_t x_row_stride, x_head_stride, out_row_stride, out_head_stride, pos_stride;
+  double theta;
+  int32_t dtype, rows, heads, head_dim, n_axes, interleaved, inverse, device;
+  int32_t sections[VS_MAX_AXES];
+} vs_rope;
+int vs_rope_axes(const vs_rope* rope, void* cuda_stream);
 
 /* A paged cache of 8-bit keys and values, the caller's memory.  Codes are e4m3 (largest 448); a
  * page's codes of one head share a scale 2^e, e in [-110, 120]: value = code * 2^e, exact in bf16. */
@@ -344,6 +349,16 @@ typedef struct {
   int32_t table_width;
   int32_t n_rows;                /* rows of the call, all sequences                                  */
   int32_t reserved;              /* 0                                                                */
+} vs_cache_seqs;
+
+/* Rows of keys and values, [n_rows][n_kv_heads][head_dim] of dtype. */
+typedef struct {
+  vs_cache_seqs seqs;
+  void* k;                       /* DEVICE, 16-byte aligned, strides multiples of 16 bytes, a head's elements side by side */
+  void* v;
+  int64_t k_row_stride, k_head_stride, v_row_stride, v_head_stride;
+  int32_t dtype;
+  int32_t reserved;              /* 0                                                                */
 } vs_cache_rows;
 
 /* Appends rows to sequences, quantising them: a page's scale is the smallest power of two with every
@@ -351,17 +366,12 @@ typedef struct {
  * ahead of the rows; where rows raise it, the codes of those tokens are rounded once more at the new scale.  A row written to
  * the first place of a page starts the page afresh.  Nearest code, ties to even; infinities become +-448, NaN stays
  * NaN.  Appending ends the sequence: codes behind its last row are left as they were and count for nothing.
- * k, v: DEVICE [n_rows][n_kv_heads][head_dim] of dtype, 16-byte aligned, strides multiples of 16 bytes.
  * No page may be written for two sequences of a call (pages that several sequences share must be full);
  * which of them is kept is not defined then. */
-int vs_cache_write(const vs_cache* cache, const vs_cache_rows* rows,
-                   const void* k, int64_t k_row_stride, int64_t k_head_stride,
-                   const void* v, int64_t v_row_stride, int64_t v_head_stride, int32_t dtype, void* cuda_stream);
+int vs_cache_write(const vs_cache* cache, const vs_cache_rows* rows, void* cuda_stream);
 
-/* Reads rows back: the values that the codes stand for, exact in either dtype. */
-int vs_cache_read(const vs_cache* cache, const vs_cache_rows* rows,
-                  void* k, int64_t k_row_stride, int64_t k_head_stride,
-                  void* v, int64_t v_row_stride, int64_t v_head_stride, int32_t dtype, void* cuda_stream);
+/* Reads rows back into k and v: the values that the codes stand for, exact in either dtype. */
+int vs_cache_read(const vs_cache* cache, const vs_cache_rows* rows, void* cuda_stream);
 
 /* Softmax attention of each sequence's rows over its tokens in the cache (Eq. 1, grouped KV heads):
  * row j of n stands at position tokens - n + j and sees the tokens that exist, with causal != 0 none
@@ -379,11 +389,19 @@ int vs_cache_read(const vs_cache* cache, const vs_cache_rows* rows,
  *      VS_ERR_DEVICE_TIMEOUT if a bounded wait of a kernel expires (the call's rows are unspecified then) and is
  *      written in no other case: clear it once. */
 int vs_cache_attention_bytes(int32_t head_dim, size_t* out_bytes);
-int vs_cache_attention(const vs_cache* cache, const vs_cache_rows* rows,
-                       const void* q, int64_t q_row_stride, int64_t q_head_stride, int32_t n_q_heads,
-                       float scale, int32_t causal, int32_t window,
-                       void* out, int64_t out_row_stride, int64_t out_head_stride, int32_t out_dtype,
-                       float* lse, void* workspace, size_t workspace_bytes, void* cuda_stream);
+typedef struct {
+  vs_cache_seqs seqs;
+  const void* q;
+  void* out;
+  float* lse;
+  void* workspace;
+  uint64_t workspace_bytes;
+  int64_t q_row_stride, q_head_stride, out_row_stride, out_head_stride;
+  int32_t n_q_heads, causal, window, out_dtype;
+  float scale;
+  int32_t reserved;              /* 0                                                                */
+} vs_cache_queries;
+int vs_cache_attention(const vs_cache* cache, const vs_cache_queries* queries, void* cuda_stream);
 
 /* What rows of logits (vs_lm_head's) say about given tokens:
  *   logprob[r] = x_t - log sum_j e^{x_j}, t = tokens[r];  entropy[r] = -sum_j p_j log p_j (nats);
@@ -391,13 +409,23 @@ int vs_cache_attention(const vs_cache* cache, const vs_cache_rows* rows,
  *   number" (0: t is vs_lm_head's next_token);  top_index, top_logprob [rows][top]: the first `top` of that order.
  * logits: DEVICE [rows][vocab] of dtype, row_stride between rows, aligned to their type (faster when rows
  *   begin on 16-byte boundaries); -inf is a token that cannot be.
- * tokens: DEVICE int32 [rows]; a negative one asks nothing (logprob 0, rank -1), one >= vocab gets NaN and -1.
+ * tokens: DEVICE int32 [rows], NULL only without logprob and rank; a negative one asks nothing (logprob 0, rank -1), one >= vocab gets NaN and -1.
  * Outputs: DEVICE, each may be NULL (top_index not when top > 0); all fp32 but rank and top_index (int32).
  * A row that holds NaN or +inf has NaN for what is summed; one of -inf only has -inf and entropy 0.
  * top: 0 .. VS_MAX_TOP, at most vocab. */
-int vs_token_logprobs(const void* logits, int64_t row_stride, int32_t dtype, int32_t rows, int32_t vocab,
-                      const int32_t* tokens, int32_t top, float* logprob, float* entropy, int32_t* rank,
-                      int32_t* top_index, float* top_logprob, int32_t device, void* cuda_stream);
+typedef struct {
+  const void* logits;
+  const int32_t* tokens;
+  float* logprob;
+  float* entropy;
+  int32_t* rank;
+  int32_t* top_index;
+  float* top_logprob;
+  int64_t row_stride;
+  int32_t dtype, rows, vocab, top, device;
+  int32_t reserved;              /* 0                                                                */
+} vs_scores;
+int vs_token_logprobs(const vs_scores* scores, void* cuda_stream);
 
 const char* vs_status_string(int status);
 

@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from typing import List, Optional, Sequence
 
 import numpy as np
@@ -70,9 +71,11 @@ class VsCache(C.Structure):
         (n, C.c_int32) for n in ("n_pages", "n_kv_heads", "head_dim", "device")]
 
 
-class VsCacheRows(C.Structure):
-    _fields_ = [(n, C.c_void_p) for n in ("page_table", "tokens", "row_offsets")] + [
-        (n, C.c_int32) for n in ("n_seqs", "table_width", "n_rows", "reserved")]
+# The argument blocks of the stand-alone operators, packed in one go: a call of one row is bound by the host.  Field by field as in the header.
+VS_ROPE = struct.Struct("3P5qd12i")
+VS_CACHE_ROWS = struct.Struct("3P4i2P4q2i")
+VS_CACHE_QUERIES = struct.Struct("3P4i4PQ4q4ifi")
+VS_SCORES = struct.Struct("7Pq6i")
 
 
 class VsError(RuntimeError):
@@ -115,13 +118,11 @@ def load_library(path: Optional[str] = None) -> C.CDLL:
     lib.vs_profile_enable.argtypes = [vp, i32, i32]
     lib.vs_profile_read.argtypes = [vp, C.POINTER(C.c_double), C.POINTER(C.c_int64), C.POINTER(C.c_int64)]
     lib.vs_evict_choose_static.argtypes = [vp, vp, i32, i32, i32, vp, vp]
-    i64, cache, rows = C.c_int64, C.POINTER(VsCache), C.POINTER(VsCacheRows)
-    lib.vs_rope_axes.argtypes = [vp, i64, i64, vp, i64, i64, i32, i32, i32, i32, vp, i64, i32, i32p, i32, i32, C.c_double, i32, vp]
-    lib.vs_cache_write.argtypes = [cache, rows, vp, i64, i64, vp, i64, i64, i32, vp]
-    lib.vs_cache_read.argtypes = [cache, rows, vp, i64, i64, vp, i64, i64, i32, vp]
+    block = C.c_char_p                                                  # (a packed argument block)
+    lib.vs_rope_axes.argtypes = [block, vp]
+    lib.vs_cache_write.argtypes = lib.vs_cache_read.argtypes = lib.vs_cache_attention.argtypes = [C.POINTER(VsCache), block, vp]
     lib.vs_cache_attention_bytes.argtypes = [i32, C.POINTER(C.c_size_t)]
-    lib.vs_cache_attention.argtypes = [cache, rows, vp, i64, i64, i32, C.c_float, i32, i32, vp, i64, i64, i32, vp, vp, C.c_size_t, vp]
-    lib.vs_token_logprobs.argtypes = [vp, i64, i32, i32, i32, vp, i32, vp, vp, vp, vp, vp, i32, vp]
+    lib.vs_token_logprobs.argtypes = [block, vp]
     lib.vs_kernel_class_name.argtypes = [i32]
     lib.vs_kernel_class_name.restype = C.c_char_p
     for name in EXPORTS:
@@ -293,16 +294,18 @@ def vs_last_step_kv(handle: int, rows: int, n_kv_heads: int, head_dim: int):
 
 
 # ---- stand-alone operators on torch tensors ------------------------------------------------------
+_torch = None
 _raw_stream = None
 
 
-def _current_stream(index: int) -> int:
-    global _raw_stream
-    import torch
-    if _raw_stream is None:
+def _need_torch():
+    global _torch, _raw_stream
+    if _torch is None:
+        import torch
         _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (      # (not part of torch's public API)
             lambda i: torch.cuda.current_stream(i).cuda_stream)
-    return _raw_stream(index)
+        _torch = torch
+    return _torch
 
 
 def _need(ok: bool, what: str) -> None:
@@ -310,39 +313,38 @@ def _need(ok: bool, what: str) -> None:
         raise ValueError(what)
 
 
-def _dtype_code(t, what: str) -> int:
-    import torch
-    if t.dtype == torch.bfloat16:
+def _dtype_code(dtype, what: str) -> int:
+    if dtype is _torch.bfloat16:
         return 0
-    _need(t.dtype == torch.float32, f"{what}: bf16 or fp32 wanted, got {t.dtype}")
+    _need(dtype is _torch.float32, what)
     return 1
 
 
-def _on(index: int, what: str, *tensors) -> None:
-    for t in tensors:
-        _need(t is None or (t.is_cuda and t.device.index == index), f"{what}: all tensors must be on cuda:{index}")
+def _on_gpu(t, what: str) -> int:
+    index = t.get_device()
+    _need(index >= 0, what)
+    return index
 
 
 def rope_axes(x, positions, sections, theta: float = 1.0e6, interleaved: bool = False, inverse: bool = False, out=None):
     """Rotary positions with several axes: ``x`` [rows, heads, head_dim] (bf16 or fp32, any row and head stride of whole 16
     bytes) turned by ``positions`` int64 [n_axes, rows]; ``sections``: pairs of each axis, head_dim / 2 in all.  ``out``:
     where to (``x`` itself turns in place); a new tensor if None.  Returns ``out``."""
-    import torch
-    _need(x.dim() == 3 and positions.dim() == 2 and positions.shape[0] == len(sections) and positions.shape[1] == x.shape[0],
-          "rope_axes: x [rows, heads, head_dim] and positions [n_axes, rows] wanted")
-    _need(positions.dtype == torch.int64 and positions.stride(1) == 1 or positions.shape[1] <= 1 and positions.dtype == torch.int64,
-          "rope_axes: positions int64, rows side by side")
-    code, index = _dtype_code(x, "rope_axes"), x.device.index
+    torch = _need_torch()
     if out is None:
         out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    _need(out.shape == x.shape and out.dtype == x.dtype and x.stride(2) == 1 and out.stride(2) == 1,
-          "rope_axes: out like x, the elements of a head side by side")
-    _on(index, "rope_axes", x, positions, out)
-    n = len(sections)
-    _check(load_library().vs_rope_axes(x.data_ptr(), x.stride(0), x.stride(1), out.data_ptr(), out.stride(0), out.stride(1), code,
-                                       x.shape[0], x.shape[1], x.shape[2], positions.data_ptr(), positions.stride(0), n,
-                                       (C.c_int32 * n)(*sections), int(interleaved), int(inverse), theta, index,
-                                       _current_stream(index) or None), "vs_rope_axes")
+    shape, step, pos_shape, pos_step, n = x.shape, x.stride(), positions.shape, positions.stride(), len(sections)
+    _need(len(shape) == 3 and pos_shape == (n, shape[0]), "rope_axes: x [rows, heads, head_dim] and positions [n_axes, rows] wanted")
+    _need(1 <= n <= VS_MAX_AXES, "rope_axes: 1 to 4 axes")
+    _need(positions.dtype is torch.int64 and (pos_step[1] == 1 or shape[0] <= 1), "rope_axes: positions int64, rows side by side")
+    out_step = step if out is x else out.stride()
+    _need(out is x or out.shape == shape and out.dtype is x.dtype, "rope_axes: out like x")
+    _need(step[2] == 1 and out_step[2] == 1, "rope_axes: the elements of a head side by side")
+    code, index = _dtype_code(x.dtype, "rope_axes: bf16 or fp32 wanted"), _on_gpu(x, "rope_axes: tensors on a GPU wanted")
+    _need(positions.get_device() == index and out.get_device() == index, "rope_axes: tensors on one GPU wanted")
+    block = VS_ROPE.pack(x.data_ptr(), out.data_ptr(), positions.data_ptr(), step[0], step[1], out_step[0], out_step[1], pos_step[0], theta,
+                         code, shape[0], shape[1], shape[2], n, interleaved, inverse, index, *sections, *((0,) * (VS_MAX_AXES - n)))
+    _check(load_library().vs_rope_axes(block, _raw_stream(index)), "vs_rope_axes")
     return out
 
 
@@ -350,30 +352,29 @@ def token_logprobs(logits, tokens=None, top: int = 0, out=None):
     """What rows of ``logits`` [rows, vocab] (fp32 or bf16) say about ``tokens`` int32 [rows] (None: nothing is asked):
     (logprob fp32 [rows], entropy fp32 [rows], rank int32 [rows], top_index int32 [rows, top], top_logprob fp32 [rows, top]);
     ``out``: such a tuple to write to."""
-    import torch
-    _need(logits.dim() == 2 and (logits.stride(1) == 1 or logits.shape[1] == 1), "token_logprobs: logits [rows, vocab], a row's side by side")
-    rows, vocab = logits.shape
-    code, index = _dtype_code(logits, "token_logprobs"), logits.device.index
-    if tokens is not None:
-        _need(tokens.dtype == torch.int32 and tokens.shape == (rows,) and tokens.is_contiguous(), "token_logprobs: tokens int32 [rows]")
+    torch = _need_torch()
+    shape, step = logits.shape, logits.stride()
+    _need(len(shape) == 2 and (step[1] == 1 or shape[1] == 1), "token_logprobs: logits [rows, vocab], a row's side by side")
+    rows, vocab = shape
+    code, index = _dtype_code(logits.dtype, "token_logprobs: fp32 or bf16 wanted"), _on_gpu(logits, "token_logprobs: tensors on a GPU wanted")
+    asked = tokens is not None
+    if asked:
+        _need(tokens.dtype is torch.int32 and tokens.shape == (rows,) and tokens.is_contiguous() and tokens.get_device() == index,
+              "token_logprobs: tokens int32 [rows]")
     if out is None:
-        real = lambda *s: torch.empty(s, dtype=torch.float32, device=logits.device)
-        whole = lambda *s: torch.empty(s, dtype=torch.int32, device=logits.device)
-        out = (real(rows), real(rows), whole(rows), whole(rows, top), real(rows, top))
+        like = dict(device=logits.device)
+        out = (torch.empty(rows, **like), torch.empty(rows, **like), torch.empty(rows, dtype=torch.int32, **like),
+               torch.empty((rows, top), dtype=torch.int32, **like), torch.empty((rows, top), **like))
     else:
-        for t, shape, dtype in zip(out, ((rows,), (rows,), (rows,), (rows, top), (rows, top)),
-                                   (torch.float32, torch.float32, torch.int32, torch.int32, torch.float32)):
-            _need(t.shape == shape and t.dtype == dtype and t.is_contiguous(), "token_logprobs: out as described")
-    _on(index, "token_logprobs", logits, tokens, *out)
+        for t, n, dtype in zip(out, (rows, rows, rows, rows * top, rows * top), (torch.float32, torch.float32, torch.int32, torch.int32, torch.float32)):
+            _need(t.numel() == n and t.dtype is dtype and t.is_contiguous() and t.get_device() == index, "token_logprobs: out as described")
     lp, entropy, rank, best, best_lp = out
-    if tokens is None and rows:
+    if not asked:
         lp.zero_()
         rank.fill_(-1)
-    asked = tokens is not None
-    _check(load_library().vs_token_logprobs(logits.data_ptr(), logits.stride(0), code, rows, vocab, tokens.data_ptr() if asked else None, top,
-                                            lp.data_ptr() if asked else None, entropy.data_ptr(), rank.data_ptr() if asked else None,
-                                            best.data_ptr() if top else None, best_lp.data_ptr() if top else None, index,
-                                            _current_stream(index) or None), "vs_token_logprobs")
+    block = VS_SCORES.pack(logits.data_ptr(), tokens.data_ptr() if asked else 0, lp.data_ptr() if asked else 0, entropy.data_ptr(),
+                           rank.data_ptr() if asked else 0, best.data_ptr(), best_lp.data_ptr(), step[0], code, rows, vocab, top, index, 0)
+    _check(load_library().vs_token_logprobs(block, _raw_stream(index)), "vs_token_logprobs")
     return out
 
 
@@ -384,13 +385,13 @@ class PageCache:
     tensors, read when the kernels run.  All methods only enqueue work on the current torch stream."""
 
     def __init__(self, k, v, k_scale, v_scale):
-        import torch
+        torch = _need_torch()
         _need(k.dim() == 4 and k.shape[2] == VS_CACHE_PAGE and v.shape == k.shape and k_scale.shape == k.shape[:2] and v_scale.shape == k.shape[:2],
               "PageCache: k, v [n_pages, n_kv_heads, 64, head_dim] and scales [n_pages, n_kv_heads] wanted")
         _need(k.dtype == v.dtype == torch.float8_e4m3fn and k_scale.dtype == v_scale.dtype == torch.float32, "PageCache: e4m3 codes, fp32 scales")
         _need(all(t.is_contiguous() for t in (k, v, k_scale, v_scale)), "PageCache: contiguous tensors wanted")
-        self.device_index = k.device.index
-        _on(self.device_index, "PageCache", k, v, k_scale, v_scale)
+        self.device_index = _on_gpu(k, "PageCache: tensors on a GPU wanted")
+        _need(all(t.get_device() == self.device_index for t in (v, k_scale, v_scale)), "PageCache: tensors on one GPU wanted")
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.n_pages, self.n_kv_heads, _, self.head_dim = k.shape
         self._cache = VsCache(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), self.n_pages, self.n_kv_heads,
@@ -399,83 +400,86 @@ class PageCache:
 
     @classmethod
     def empty(cls, n_pages: int, n_kv_heads: int, head_dim: int, device=0) -> "PageCache":
-        import torch
+        """A cache of its own, all zeros."""
+        torch = _need_torch()
         dev = torch.device("cuda", device)
         codes = lambda: torch.zeros((n_pages, n_kv_heads, VS_CACHE_PAGE, head_dim), dtype=torch.uint8, device=dev).view(torch.float8_e4m3fn)
         scales = lambda: torch.zeros((n_pages, n_kv_heads), dtype=torch.float32, device=dev)
         return cls(codes(), codes(), scales(), scales())
 
-    def _rows(self, what, page_table, tokens, row_offsets, n_rows):
-        import torch
-        n = page_table.shape[0]
-        _need(page_table.dim() == 2 and page_table.dtype == torch.int32 and page_table.is_contiguous(), f"{what}: page_table int32 [n_seqs, table_width]")
-        _need(tokens.dtype == torch.int32 and tokens.shape == (n,) and tokens.is_contiguous(), f"{what}: one int32 a sequence")
-        _need(row_offsets is None or (row_offsets.dtype == torch.int32 and row_offsets.shape == (n + 1,) and row_offsets.is_contiguous()),
-              f"{what}: row_offsets int32 [n_seqs + 1]")
-        _on(self.device_index, what, page_table, tokens, row_offsets)
-        return VsCacheRows(page_table.data_ptr(), tokens.data_ptr(), row_offsets.data_ptr() if row_offsets is not None else None, n,
-                           page_table.shape[1], n_rows, 0)
+    def _seqs(self, page_table, tokens, row_offsets):
+        """Pointers and sizes of a call's sequences, checked."""
+        i32, index, shape = _torch.int32, self.device_index, page_table.shape
+        _need(len(shape) == 2 and page_table.dtype is i32 and page_table.is_contiguous() and page_table.get_device() == index,
+              "PageCache: page_table int32 [n_seqs, table_width], on the cache's GPU")
+        n, width = shape
+        _need(tokens.numel() == n and tokens.dtype is i32 and tokens.is_contiguous() and tokens.get_device() == index,
+              "PageCache: start / lengths int32 [n_seqs], on the cache's GPU")
+        if row_offsets is None:
+            return page_table.data_ptr(), tokens.data_ptr(), 0, n, width
+        _need(row_offsets.numel() == n + 1 and row_offsets.dtype is i32 and row_offsets.is_contiguous() and row_offsets.get_device() == index,
+              "PageCache: row_offsets int32 [n_seqs + 1], on the cache's GPU")
+        return page_table.data_ptr(), tokens.data_ptr(), row_offsets.data_ptr(), n, width
 
-    def _kv(self, what, k, v):
-        _need(k.dim() == 3 and k.shape == v.shape and k.shape[1:] == (self.n_kv_heads, self.head_dim) and k.dtype == v.dtype,
-              f"{what}: k, v [n_rows, n_kv_heads, head_dim] wanted")
-        _need(k.stride(2) == 1 and v.stride(2) == 1, f"{what}: the elements of a head side by side")
-        _on(self.device_index, what, k, v)
-        return _dtype_code(k, what)
+    def _kv(self, page_table, start, k, v, row_offsets):
+        shape, ks, vs, dtype = k.shape, k.stride(), v.stride(), k.dtype
+        _need(len(shape) == 3 and v.shape == shape and shape[1] == self.n_kv_heads and shape[2] == self.head_dim and v.dtype is dtype,
+              "PageCache: k, v [n_rows, n_kv_heads, head_dim] wanted")
+        _need(ks[2] == 1 and vs[2] == 1, "PageCache: the elements of a head side by side")
+        _need(k.get_device() == self.device_index and v.get_device() == self.device_index, "PageCache: k, v on the cache's GPU")
+        return VS_CACHE_ROWS.pack(*self._seqs(page_table, start, row_offsets), shape[0], 0, k.data_ptr(), v.data_ptr(), ks[0], ks[1], vs[0], vs[1],
+                                  _dtype_code(dtype, "PageCache: rows of bf16 or fp32 wanted"), 0)
 
     def write(self, page_table, start, k, v, row_offsets=None):
         """Appends rows [n_rows, n_kv_heads, head_dim] (bf16 or fp32): sequence i's from its token ``start[i]`` on."""
-        code, rows = self._kv("write", k, v), self._rows("write", page_table, start, row_offsets, k.shape[0])
-        _check(load_library().vs_cache_write(self._cache, rows, k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(), v.stride(0), v.stride(1),
-                                             code, _current_stream(self.device_index) or None), "vs_cache_write")
+        _check(load_library().vs_cache_write(self._cache, self._kv(page_table, start, k, v, row_offsets), _raw_stream(self.device_index)),
+               "vs_cache_write")
 
     def read(self, page_table, start, k, v, row_offsets=None):
         """Reads rows back into k, v [n_rows, n_kv_heads, head_dim] (bf16 or fp32); returns them."""
-        code, rows = self._kv("read", k, v), self._rows("read", page_table, start, row_offsets, k.shape[0])
-        _check(load_library().vs_cache_read(self._cache, rows, k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(), v.stride(0), v.stride(1),
-                                            code, _current_stream(self.device_index) or None), "vs_cache_read")
+        _check(load_library().vs_cache_read(self._cache, self._kv(page_table, start, k, v, row_offsets), _raw_stream(self.device_index)),
+               "vs_cache_read")
         return k, v
 
     def workspace(self):
         """A workspace for ``attend``; two calls that may overlap (graphs replayed side by side) need one each."""
-        import torch
         out = C.c_size_t(0)
         _check(load_library().vs_cache_attention_bytes(self.head_dim, C.byref(out)), "vs_cache_attention_bytes")
-        workspace = torch.empty(out.value, dtype=torch.uint8, device=self.k.device)
+        workspace = _torch.empty(out.value, dtype=_torch.uint8, device=self.k.device)
         workspace[:256].zero_()
         return workspace
 
     def attend_status(self) -> int:
         """0, or VS_ERR_DEVICE_TIMEOUT if a wait of an ``attend`` with one of the cache's own workspaces ever ran out.  Synchronises."""
-        import torch
-        return min([int(w[:4].view(torch.int32).item()) for w in self._workspaces.values()], default=VS_OK)
+        return min([int(w[:4].view(_torch.int32).item()) for w in self._workspaces.values()], default=VS_OK)
 
     def attend(self, page_table, lengths, q, out=None, lse=None, row_offsets=None, scale=None, causal=True, window=0, workspace=None,
                out_dtype=None):
         """Attention of q bf16 [n_rows, n_q_heads, head_dim] over each sequence's ``lengths[i]`` tokens, its rows counted in.
         -> (out [n_rows, n_q_heads, head_dim], lse fp32 [n_rows, n_q_heads]).  ``out_dtype``: of a new ``out``, bf16 or fp32.  Without
         ``workspace`` the cache keeps one for every stream it is used on."""
-        import torch
-        _need(q.dim() == 3 and q.dtype == torch.bfloat16 and q.shape[2] == self.head_dim and q.stride(2) == 1,
-              "attend: q bf16 [n_rows, n_q_heads, head_dim]")
-        n_rows, n_heads = q.shape[0], q.shape[1]
+        torch, index = _torch, self.device_index
+        shape, step = q.shape, q.stride()
+        _need(len(shape) == 3 and q.dtype is torch.bfloat16 and shape[2] == self.head_dim and step[2] == 1 and q.get_device() == index,
+              "attend: q bf16 [n_rows, n_q_heads, head_dim], on the cache's GPU")
+        n_rows, n_heads, head_dim = shape
         if out is None:
-            out = torch.empty(q.shape, dtype=out_dtype or torch.bfloat16, device=q.device)
+            out = torch.empty(shape, dtype=out_dtype or torch.bfloat16, device=q.device)
         if lse is None:
             lse = torch.empty((n_rows, n_heads), dtype=torch.float32, device=q.device)
-        _need(out.shape == q.shape and out.stride(2) == 1, "attend: out like q")
-        _need(lse.shape == (n_rows, n_heads) and lse.dtype == torch.float32 and lse.is_contiguous(), "attend: lse fp32 [n_rows, n_q_heads]")
-        code, rows = _dtype_code(out, "attend"), self._rows("attend", page_table, lengths, row_offsets, n_rows)
-        _on(self.device_index, "attend", q, out, lse, workspace)
-        stream = _current_stream(self.device_index)
+        out_step = out.stride()
+        _need(out.shape == shape and out_step[2] == 1 and out.get_device() == index, "attend: out like q")
+        _need(lse.numel() == n_rows * n_heads and lse.dtype is torch.float32 and lse.is_contiguous() and lse.get_device() == index,
+              "attend: lse fp32 [n_rows, n_q_heads]")
+        stream = _raw_stream(index)
         if workspace is None:
             workspace = self._workspaces.get(stream)
             if workspace is None:
                 workspace = self._workspaces[stream] = self.workspace()
-        _check(load_library().vs_cache_attention(self._cache, rows, q.data_ptr(), q.stride(0), q.stride(1), n_heads,
-                                                 self.head_dim ** -0.5 if scale is None else scale, int(causal), window, out.data_ptr(),
-                                                 out.stride(0), out.stride(1), code, lse.data_ptr(), workspace.data_ptr(), workspace.numel(),
-                                                 stream or None), "vs_cache_attention")
+        block = VS_CACHE_QUERIES.pack(*self._seqs(page_table, lengths, row_offsets), n_rows, 0, q.data_ptr(), out.data_ptr(), lse.data_ptr(),
+                                      workspace.data_ptr(), workspace.nbytes, step[0], step[1], out_step[0], out_step[1], n_heads, causal, window,
+                                      _dtype_code(out.dtype, "attend: out of bf16 or fp32 wanted"), head_dim ** -0.5 if scale is None else scale, 0)
+        _check(load_library().vs_cache_attention(self._cache, block, stream), "vs_cache_attention")
         return out, lse
 
 

@@ -19,15 +19,15 @@ constexpr int kThreads = 256;
 
 struct CacheArgs {
   vs_cache c;
-  vs_cache_rows r;
-  const void *k, *v;                  // rows; written to by the reading kernel
+  vs_cache_seqs r;
+  void *k, *v;                        // rows
   long long k_row, k_head, v_row, v_head;
 };
 
 // The `unit`-th page that the call's rows lie in, counted through the sequences: rows [row, row + n) are tokens at ... at + n - 1
 // of the page.
 struct PageRows { int seq, page, at, row, n; };
-__device__ __forceinline__ PageRows find_page(const vs_cache_rows& r, int n_pages, int unit) {
+__device__ __forceinline__ PageRows find_page(const vs_cache_seqs& r, int n_pages, int unit) {
   const int lane = threadIdx.x & 31;
   PageRows found = {-1, -1, 0, 0, 0};
   long long before = 0;
@@ -129,7 +129,7 @@ __global__ void __launch_bounds__(kThreads) cache_read_kernel(const __grid_const
   const PageRows p = find_page(a.r, a.c.n_pages, (int)blockIdx.x);
   if (p.n == 0) return;
   const int head = (int)blockIdx.y >> 1, is_v = (int)blockIdx.y & 1;
-  T* rows = static_cast<T*>(const_cast<void*>(is_v ? a.v : a.k)) + (long long)p.row * (is_v ? a.v_row : a.k_row) + (long long)head * (is_v ? a.v_head : a.k_head);
+  T* rows = static_cast<T*>(is_v ? a.v : a.k) + (long long)p.row * (is_v ? a.v_row : a.k_row) + (long long)head * (is_v ? a.v_head : a.k_head);
   const long long step = is_v ? a.v_row : a.k_row;
   const size_t tile = (size_t)max(p.page, 0) * a.c.n_kv_heads + head;
   const uint8_t* codes = static_cast<const uint8_t*>(is_v ? a.c.v : a.c.k) + tile * (kPage * D);
@@ -155,18 +155,20 @@ __global__ void __launch_bounds__(kThreads) cache_read_kernel(const __grid_const
   }
 }
 
-int run(const vs_cache* c, const vs_cache_rows* r, const void* k, int64_t k_row, int64_t k_head, const void* v, int64_t v_row, int64_t v_head,
-        int32_t dtype, void* cuda_stream, bool write) {
+int run(const vs_cache* c, const vs_cache_rows* rows, void* cuda_stream, bool write) {
+  if (rows == nullptr) return VS_ERR_INVALID_ARG;
+  const vs_cache_seqs* r = &rows->seqs;
   const int rc = check_cache(c, r);
   if (rc != VS_OK) return rc;
+  const int32_t dtype = rows->dtype;
   if (dtype < 0 || dtype > 1) return VS_ERR_INVALID_ARG;
   if (r->n_rows == 0) return VS_OK;
-  if (k == nullptr || v == nullptr || !aligned(k, 16) || !aligned(v, 16)) return VS_ERR_INVALID_ARG;
-  const int64_t piece = dtype == 1 ? 4 : 8, strides[4] = {k_row, k_head, v_row, v_head};
+  if (rows->k == nullptr || rows->v == nullptr || !aligned(rows->k, 16) || !aligned(rows->v, 16)) return VS_ERR_INVALID_ARG;
+  const int64_t piece = dtype == 1 ? 4 : 8, strides[4] = {rows->k_row_stride, rows->k_head_stride, rows->v_row_stride, rows->v_head_stride};
   for (int64_t s : strides) if (s % piece != 0) return VS_ERR_INVALID_ARG;
   OnDevice on(c->device);
   if (!on.ok) return VS_ERR_CUDA;
-  CacheArgs a = {*c, *r, k, v, k_row, k_head, v_row, v_head};
+  CacheArgs a = {*c, *r, rows->k, rows->v, strides[0], strides[1], strides[2], strides[3]};
   // most pages that the rows can lie in: a sequence's first and last one are perhaps not full
   const long long pages = (long long)r->n_rows / kPage + 2ll * r->n_seqs;
   const dim3 grid((unsigned)(pages < r->n_rows ? pages : r->n_rows), (unsigned)(2 * c->n_kv_heads));
@@ -189,12 +191,5 @@ int run(const vs_cache* c, const vs_cache_rows* r, const void* k, int64_t k_row,
 
 }  // namespace vs
 
-extern "C" int vs_cache_write(const vs_cache* cache, const vs_cache_rows* rows, const void* k, int64_t k_row_stride, int64_t k_head_stride,
-                              const void* v, int64_t v_row_stride, int64_t v_head_stride, int32_t dtype, void* cuda_stream) {
-  return vs::run(cache, rows, k, k_row_stride, k_head_stride, v, v_row_stride, v_head_stride, dtype, cuda_stream, true);
-}
-
-extern "C" int vs_cache_read(const vs_cache* cache, const vs_cache_rows* rows, void* k, int64_t k_row_stride, int64_t k_head_stride,
-                             void* v, int64_t v_row_stride, int64_t v_head_stride, int32_t dtype, void* cuda_stream) {
-  return vs::run(cache, rows, k, k_row_stride, k_head_stride, v, v_row_stride, v_head_stride, dtype, cuda_stream, false);
-}
+extern "C" int vs_cache_write(const vs_cache* cache, const vs_cache_rows* rows, void* cuda_stream) { return vs::run(cache, rows, cuda_stream, true); }
+extern "C" int vs_cache_read(const vs_cache* cache, const vs_cache_rows* rows, void* cuda_stream) { return vs::run(cache, rows, cuda_stream, false); }

@@ -478,35 +478,34 @@ extern "C" int vs_cache_attention_bytes(int32_t head_dim, size_t* out_bytes) {
   return VS_OK;
 }
 
-extern "C" int vs_cache_attention(const vs_cache* cache, const vs_cache_rows* rows, const void* q, int64_t q_row_stride, int64_t q_head_stride,
-                                  int32_t n_q_heads, float scale, int32_t causal, int32_t window, void* out, int64_t out_row_stride,
-                                  int64_t out_head_stride, int32_t out_dtype, float* lse, void* workspace, size_t workspace_bytes,
-                                  void* cuda_stream) {
+extern "C" int vs_cache_attention(const vs_cache* cache, const vs_cache_queries* x, void* cuda_stream) {
   using namespace vs;
+  if (x == nullptr) return VS_ERR_INVALID_ARG;
+  const vs_cache_seqs* rows = &x->seqs;
   const int rc = check_cache(cache, rows);
   if (rc != VS_OK) return rc;
-  if (n_q_heads < 1 || window < 0 || out_dtype < 0 || out_dtype > 1 || !(scale > 0.f) || !std::isfinite(scale)) return VS_ERR_INVALID_ARG;
-  if (n_q_heads % cache->n_kv_heads != 0 || n_q_heads / cache->n_kv_heads > 8) return VS_ERR_UNSUPPORTED;
-  const int G = n_q_heads / cache->n_kv_heads;
+  if (x->n_q_heads < 1 || x->window < 0 || x->out_dtype < 0 || x->out_dtype > 1 || !(x->scale > 0.f) || !std::isfinite(x->scale)) return VS_ERR_INVALID_ARG;
+  if (x->n_q_heads % cache->n_kv_heads != 0 || x->n_q_heads / cache->n_kv_heads > 8) return VS_ERR_UNSUPPORTED;
+  const int G = x->n_q_heads / cache->n_kv_heads;
   if (rows->n_rows > (1 << 27)) return VS_ERR_UNSUPPORTED;
   size_t need = 0;
   vs_cache_attention_bytes(cache->head_dim, &need);
   if (rows->n_rows == 0) return VS_OK;
-  if (q == nullptr || out == nullptr || workspace == nullptr) return VS_ERR_INVALID_ARG;
-  if (workspace_bytes < need) return VS_ERR_CAPACITY;
-  if (!aligned(q, 16) || !aligned(out, out_dtype == 1 ? 16 : 8) || !aligned(workspace, 256) || !aligned(lse, 4)) return VS_ERR_INVALID_ARG;
-  if (q_row_stride % 8 != 0 || q_head_stride % 8 != 0 || out_row_stride % 4 != 0 || out_head_stride % 4 != 0) return VS_ERR_INVALID_ARG;
+  if (x->q == nullptr || x->out == nullptr || x->workspace == nullptr) return VS_ERR_INVALID_ARG;
+  if (x->workspace_bytes < need) return VS_ERR_CAPACITY;
+  if (!aligned(x->q, 16) || !aligned(x->out, x->out_dtype == 1 ? 16 : 8) || !aligned(x->workspace, 256) || !aligned(x->lse, 4)) return VS_ERR_INVALID_ARG;
+  if (x->q_row_stride % 8 != 0 || x->q_head_stride % 8 != 0 || x->out_row_stride % 4 != 0 || x->out_head_stride % 4 != 0) return VS_ERR_INVALID_ARG;
   OnDevice on(cache->device);
   if (!on.ok) return VS_ERR_CUDA;
   CacheAttnArgs a = {};
   a.c = *cache; a.r = *rows;
-  a.q = static_cast<const bf16*>(q); a.out = out; a.lse = lse;
-  a.status = static_cast<int*>(workspace);
-  a.joins = reinterpret_cast<int4*>(static_cast<uint8_t*>(workspace) + kJoinsAt);
-  a.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + kPartsAt);
-  a.q_row = q_row_stride; a.q_head = q_head_stride; a.out_row = out_row_stride; a.out_head = out_head_stride;
-  a.scale_log2e = scale * 1.4426950408889634f;
-  a.Hq = n_q_heads; a.G = G; a.causal = causal != 0; a.window = window; a.out_fp32 = out_dtype;
+  a.q = static_cast<const bf16*>(x->q); a.out = x->out; a.lse = x->lse;
+  a.status = static_cast<int*>(x->workspace);
+  a.joins = reinterpret_cast<int4*>(static_cast<uint8_t*>(x->workspace) + kJoinsAt);
+  a.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(x->workspace) + kPartsAt);
+  a.q_row = x->q_row_stride; a.q_head = x->q_head_stride; a.out_row = x->out_row_stride; a.out_head = x->out_head_stride;
+  a.scale_log2e = x->scale * 1.4426950408889634f;
+  a.Hq = x->n_q_heads; a.G = G; a.causal = x->causal != 0; a.window = x->window; a.out_fp32 = x->out_dtype;
   // Which sequences have few rows the device knows; the host, from the number of rows, that all of them have (or none, where they have the
   // same number each).
   const bool uniform = rows->row_offsets == nullptr;

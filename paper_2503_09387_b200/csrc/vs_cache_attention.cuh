@@ -9,7 +9,7 @@ constexpr int kFewCtas = 3 * 148, kManyCtas = 148, kManyWide = 256;
 
 struct CacheAttnArgs {
   vs_cache c;
-  vs_cache_rows r;
+  vs_cache_seqs r;
   const bf16* q;
   void* out;
   float* lse;                     // [n_rows][Hq], or null

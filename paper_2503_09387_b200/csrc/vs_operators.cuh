@@ -29,7 +29,7 @@ constexpr int kPage = VS_CACHE_PAGE;
 constexpr int kScaleMinExp = -110, kScaleMaxExp = 120;
 
 // The checks that the calls on a cache share.
-inline int check_cache(const vs_cache* c, const vs_cache_rows* r) {
+inline int check_cache(const vs_cache* c, const vs_cache_seqs* r) {
   if (c == nullptr || r == nullptr || c->k == nullptr || c->v == nullptr || c->k_scale == nullptr || c->v_scale == nullptr) return VS_ERR_INVALID_ARG;
   if (r->page_table == nullptr || r->tokens == nullptr) return VS_ERR_INVALID_ARG;
   if (c->n_pages < 1 || c->n_kv_heads < 1 || r->table_width < 1 || r->n_rows < 0 || r->n_seqs < 1) return VS_ERR_INVALID_ARG;
@@ -45,13 +45,13 @@ inline int check_cache(const vs_cache* c, const vs_cache_rows* r) {
 #ifdef __CUDACC__
 // Rows [first, first + n) of the call are sequence i's.  Whatever the offsets hold, the rows named lie in [0, n_rows).
 struct SeqRows { int first, n; };
-__device__ __forceinline__ SeqRows rows_of(const vs_cache_rows& r, int i) {
+__device__ __forceinline__ SeqRows rows_of(const vs_cache_seqs& r, int i) {
   if (r.row_offsets == nullptr) { const int n = r.n_rows / r.n_seqs; return {i * n, n}; }
   const int a = min(max(r.row_offsets[i], 0), r.n_rows), b = min(max(r.row_offsets[i + 1], a), r.n_rows);
   return {a, b - a};
 }
 // Page of tokens 64 p ... 64 p + 63 of sequence i; -1 where the table has none that the pool holds.
-__device__ __forceinline__ int page_of(const vs_cache_rows& r, int n_pages, int i, int p) {
+__device__ __forceinline__ int page_of(const vs_cache_seqs& r, int n_pages, int i, int p) {
   if (p < 0 || p >= r.table_width) return -1;
   const int page = r.page_table[(size_t)i * r.table_width + p];
   return page >= 0 && page < n_pages ? page : -1;

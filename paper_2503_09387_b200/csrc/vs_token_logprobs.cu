@@ -4,9 +4,10 @@
 //   lse = log sum_j e^{x_j},   logprob = x_t - lse,   entropy = lse - sum_j p_j x_j,   p_j = e^{x_j - lse}
 //   rank = how many tokens come before t in the order "larger logit, else lower index"; alternatives: the first `top` of that order.
 //
-// One pass over the row with a running maximum m per thread:  s = sum of e^{x - m} over x < m,  c = how many x = m,
-// u = sum of (x - m) e^{x - m};  then log sum = log c + log1p(s / c) and entropy = that - u / (s + c).  (With the maxima counted and not
-// summed a row that is all but certain keeps the few bits that its entropy has.)
+// One pass over the row.  A thread keeps the largest logit that it has met apart and sums the others, each new one or the largest that it takes
+// the place of:  s = sum of e^{y - ref},  u = sum of (y - ref) e^{y - ref};  ref is its first logits' maximum, moved only when the largest is far above it.
+// With M the row's largest and s, u relative to it,  log sum = log1p(s)  and  entropy = that - u / (1 + s):  a row that is all but certain
+// keeps the few bits that its entropy has, and nothing in the loop branches on a new maximum.
 // Alternatives: the k-th largest of the threads' own maxima is a bound that at least k logits reach, so only threads whose maximum reaches
 // it hold any of the best k.  Their logits -- a few dozen threads' -- are read once more (they lie in L2), those that reach the bound collected and put in
 // order by counting.
@@ -34,31 +35,27 @@ struct ScoreArgs {
   int rows, vocab, top, cluster;
 };
 
-// what is known of a stretch of a row
+// what is known of a stretch of a row: its largest logit, and sums over the others relative to it
 struct Part {
-  float m, s, u;                       // (m = -inf: nothing but -inf so far)
-  uint32_t c;
+  float m, s, u;                       // (m = -inf: nothing but -inf, or nothing, so far; s = u = 0 then)
+  uint32_t pad;
   __device__ __forceinline__ void join(const Part& o) {
-    const float M = fmaxf(m, o.m);
-    if (M == -INFINITY) { c += o.c; return; }
-    const float da = m - M, db = o.m - M;                              // (-inf: that side is empty)
-    const float ra = da == -INFINITY ? 0.f : exp2f(da * kLog2e), rb = db == -INFINITY ? 0.f : exp2f(db * kLog2e);
-    const float sa = da == 0.f ? s : (s + (float)c) * ra, sb = db == 0.f ? o.s : (o.s + (float)o.c) * rb;
-    const float ua = da == 0.f ? u : (ra > 0.f ? ra * (u + da * (s + (float)c)) : 0.f);
-    const float ub = db == 0.f ? o.u : (rb > 0.f ? rb * (o.u + db * (o.s + (float)o.c)) : 0.f);
-    c = (da == 0.f ? c : 0u) + (db == 0.f ? o.c : 0u);
-    s = sa + sb;
-    u = ua + ub;
+    const float M = fmaxf(m, o.m), low = fminf(m, o.m);
+    if (low == -INFINITY) { if (m != M) *this = o; return; }
+    // the smaller of the largest joins the others
+    const float d = fmaxf(low - M, -1000.f), r = ex2_approx(d * kLog2e);
+    const float ls = m == M ? o.s : s, lu = m == M ? o.u : u, hs = m == M ? s : o.s, hu = m == M ? u : o.u;
+    s = hs + r * (1.f + ls);
+    u = hu + (r > 0.f ? r * (lu + d * (1.f + ls)) : 0.f);
     m = M;
   }
-  // over the lanes of every aligned group of `n` (the same in each of them: both sides' sums are the same two numbers added)
+  // over the lanes of every aligned group of `n`
   __device__ __forceinline__ void join_lanes(int n) {
     for (int o = n >> 1; o > 0; o >>= 1) {
       Part q;
       q.m = __shfl_xor_sync(0xffffffffu, m, o);
       q.s = __shfl_xor_sync(0xffffffffu, s, o);
       q.u = __shfl_xor_sync(0xffffffffu, u, o);
-      q.c = __shfl_xor_sync(0xffffffffu, c, o);
       join(q);
     }
   }
@@ -136,8 +133,8 @@ __global__ void __launch_bounds__(kThreads, 2) token_logprobs_kernel(const __gri
   }
   const bool xt_nan = xt != xt;
 
-  // ---- one pass: running maximum, sums, place of the token --------------------------------------------------
-  Part p = {-INFINITY, 0.f, 0.f, 0u};
+  // ---- one pass: largest, sums of the others, place of the token -----------------------------------------------
+  float best_x = -INFINITY, ref = 0.f, sum = 0.f, sum_u = 0.f;         // ref: the thread's reference
   int n_before = 0;
   bool odd = false;
   for (int v = v0 + tid; v < v1; v += U * kThreads) {
@@ -148,64 +145,51 @@ __global__ void __launch_bounds__(kThreads, 2) token_logprobs_kernel(const __gri
       const int w = v + (U + j) * kThreads;
       next[j] = w < v1 ? fetch<T, kVector>(row, w, a.vocab) : nothing;
     }
-    float x[E];
-    float most = -INFINITY;
+    const float was = best_x;
+    bool ties = false;
+    float y[E];                                                         // what is summed: the logit, or the largest so far that it replaces
 #pragma unroll
-    for (int j = 0; j < U; ++j)
-#pragma unroll
-      for (int e = 0; e < V; ++e) { x[j * V + e] = element<T>(now[j], e); most = fmaxf(most, x[j * V + e]); }
-    // the order: x > xt, or equal with a lower index
-#pragma unroll
-    for (int j = 0; j < U; ++j) {
-      const int i0 = (v + j * kThreads) * V;
-#pragma unroll
-      for (int e = 0; e < V; ++e) {
-        const float y = x[j * V + e];
-        const bool tie = y == xt && i0 + e < token;
-        n_before += (y > xt || tie) ? 1 : 0;
-      }
+    for (int i = 0; i < E; ++i) {
+      const float x = element<T>(now[i / V], i % V);
+      y[i] = fminf(best_x, x);
+      best_x = fmaxf(best_x, x);
+      n_before += x > xt ? 1 : 0;
+      ties = ties || x == xt;
+      odd = odd || !(x <= 3.402823466e38f);                            // NaN or +inf
     }
-    if (xt_nan) {
+    if (ties) {                                                        // equal ones of a lower index
 #pragma unroll
-      for (int j = 0; j < U; ++j)
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-          const int i = (v + j * kThreads) * V + e;
-          n_before += (v + j * kThreads < v1 && i < a.vocab && (x[j * V + e] == x[j * V + e] || i < token)) ? 1 : 0;
-        }
+      for (int i = 0; i < E; ++i) n_before += element<T>(now[i / V], i % V) == xt && (v + (i / V) * kThreads) * V + i % V < token ? 1 : 0;
     }
-#pragma unroll
-    for (int i = 0; i < E; ++i) odd = odd || !(x[i] <= 3.402823466e38f);      // NaN or +inf
-    if (most >= p.m) {
-      if (most > p.m) {
-        if (p.m != -INFINITY) {
-          const float d = p.m - most, r = exp2f(d * kLog2e);
-          p.u = r > 0.f ? r * (p.u + d * (p.s + (float)p.c)) : 0.f;
-          p.s = (p.s + (float)p.c) * r;
-        }
-        p.c = 0u;
-        p.m = most;
-      }
-      if (most == -INFINITY) continue;
+    if (xt_nan) {                                                      // behind every number, and NaN of a lower index
 #pragma unroll
       for (int i = 0; i < E; ++i) {
-        const float d = fmaxf(x[i] - p.m, -1000.f);                     // (-inf: 2^-1443 = 0, and 0 in u)
-        const float e = d < 0.f ? exp2f(d * kLog2e) : 0.f;
-        p.c += d < 0.f ? 0u : 1u;
-        p.s += e;
-        p.u = fmaf(d, e, p.u);
+        const int w = v + (i / V) * kThreads, at = w * V + i % V;
+        const float x = element<T>(now[i / V], i % V);
+        n_before += w < v1 && at < a.vocab && (x == x || at < token) ? 1 : 0;
       }
-    } else {
-      float s = 0.f, u = 0.f;
-#pragma unroll
-      for (int i = 0; i < E; ++i) {
-        const float d = fmaxf(x[i] - p.m, -1000.f), e = exp2f(d * kLog2e);
-        s += e;
-        u = fmaf(d, e, u);
-      }
-      p.s += s;
-      p.u += u;
     }
+    if (best_x > -INFINITY && (was == -INFINITY || best_x - ref > 40.f)) {
+      const float d = fmaxf(ref - best_x, -1000.f), r = was == -INFINITY ? 0.f : exp2f(d * kLog2e);
+      sum_u = r > 0.f ? r * (sum_u + d * sum) : 0.f;
+      sum *= r;
+      ref = best_x;
+    }
+    float s = 0.f, u = 0.f;
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+      const float d = fmaxf(y[i] - ref, -1000.f), e = ex2_approx(d * kLog2e);           // (-inf: 0, and 0 in u)
+      s += e;
+      u = fmaf(d, e, u);
+    }
+    sum += s;
+    sum_u += u;
+  }
+  Part p = {best_x, 0.f, 0.f, 0u};
+  if (best_x > -INFINITY) {
+    const float d = ref - best_x, r = exp2f(d * kLog2e);               // (e^{-40} at least)
+    p.s = sum * r;
+    p.u = r * (sum_u + d * sum);
   }
   const uint32_t own_max = ordered(p.m);
   p.join_lanes(32);
@@ -314,7 +298,7 @@ __global__ void __launch_bounds__(kThreads, 2) token_logprobs_kernel(const __gri
         if (lane < C) {
           const uint32_t at = map_shared_rank(smem_u32(&sm.whole), (uint32_t)lane), counts = map_shared_rank(smem_u32(&sm.n_before), (uint32_t)lane);
           const unsigned long long w0 = ld_peer_u64(at), w1 = ld_peer_u64(at + 8), w2 = ld_peer_u64(counts);
-          sm.part[lane] = {__uint_as_float((uint32_t)w0), __uint_as_float((uint32_t)(w0 >> 32)), __uint_as_float((uint32_t)w1), (uint32_t)(w1 >> 32)};
+          sm.part[lane] = {__uint_as_float((uint32_t)w0), __uint_as_float((uint32_t)(w0 >> 32)), __uint_as_float((uint32_t)w1), 0u};
           sm.before[lane] = (int)(uint32_t)w2;
           sm.odd[lane] = (int)(w2 >> 32);
         }
@@ -353,13 +337,13 @@ __global__ void __launch_bounds__(kThreads, 2) token_logprobs_kernel(const __gri
     bad = __any_sync(0xffffffffu, sm.odd[lane & (C - 1)] != 0);
   }
   const float nan = __int_as_float(0x7fc00000);
-  const float log_sum = logf((float)whole.c) + log1pf(whole.s / (float)whole.c);          // of e^{x - m}
+  const float log_sum = log1pf(whole.s);                                // of e^{x - m}
   const bool empty = whole.m == -INFINITY;                              // nothing but -inf (and NaN)
   auto logprob_of = [&](float x) { return bad ? nan : (empty ? -INFINITY : (x - whole.m) - log_sum); };
   if (tid == 0) {
     if (a.logprob != nullptr) a.logprob[row_i] = has_token ? logprob_of(xt) : (token < 0 ? 0.f : nan);
     if (a.rank != nullptr) a.rank[row_i] = has_token ? all_before : -1;
-    if (a.entropy != nullptr) a.entropy[row_i] = bad ? nan : (empty ? 0.f : fmaxf(log_sum - whole.u / (whole.s + (float)whole.c), 0.f));
+    if (a.entropy != nullptr) a.entropy[row_i] = bad ? nan : (empty ? 0.f : fmaxf(log_sum - whole.u / (1.f + whole.s), 0.f));
   }
   if (tid < k) {
     const int i = 0x7fffffff - (int)(uint32_t)best[tid];
@@ -391,28 +375,26 @@ int launch(const ScoreArgs& a, cudaStream_t st) {
 
 }  // namespace vs
 
-extern "C" int vs_token_logprobs(const void* logits, int64_t row_stride, int32_t dtype, int32_t rows, int32_t vocab, const int32_t* tokens,
-                                 int32_t top, float* logprob, float* entropy, int32_t* rank, int32_t* top_index, float* top_logprob,
-                                 int32_t device, void* cuda_stream) {
+extern "C" int vs_token_logprobs(const vs_scores* x, void* cuda_stream) {
   using namespace vs;
-  if (rows < 0 || vocab < 1 || dtype < 0 || dtype > 1 || top < 0) return VS_ERR_INVALID_ARG;
-  if (vocab > (1 << 30) || rows > (1 << 27)) return VS_ERR_UNSUPPORTED;
-  if (top > VS_MAX_TOP) return VS_ERR_CAPACITY;
-  if (top > vocab || (top > 0 && top_index == nullptr)) return VS_ERR_INVALID_ARG;
-  if ((logprob != nullptr || rank != nullptr) && rows > 0 && tokens == nullptr) return VS_ERR_INVALID_ARG;
-  if (rows == 0) return VS_OK;
-  const size_t el = dtype == 1 ? 4 : 2;
-  if (logits == nullptr || !aligned(logits, el) || !aligned(tokens, 4) || !aligned(logprob, 4) || !aligned(entropy, 4) || !aligned(rank, 4) ||
-      !aligned(top_index, 4) || !aligned(top_logprob, 4))
-    return VS_ERR_INVALID_ARG;
-  OnDevice on(device);
+  if (x == nullptr || x->rows < 0 || x->vocab < 1 || x->dtype < 0 || x->dtype > 1 || x->top < 0) return VS_ERR_INVALID_ARG;
+  if (x->vocab > (1 << 30) || x->rows > (1 << 27)) return VS_ERR_UNSUPPORTED;
+  if (x->top > VS_MAX_TOP) return VS_ERR_CAPACITY;
+  if (x->top > x->vocab || (x->top > 0 && x->top_index == nullptr)) return VS_ERR_INVALID_ARG;
+  if (x->rows == 0) return VS_OK;
+  if ((x->logprob != nullptr || x->rank != nullptr) && x->tokens == nullptr) return VS_ERR_INVALID_ARG;
+  const size_t el = x->dtype == 1 ? 4 : 2;
+  if (x->logits == nullptr || !aligned(x->logits, el)) return VS_ERR_INVALID_ARG;
+  const void* words[6] = {x->tokens, x->logprob, x->entropy, x->rank, x->top_index, x->top_logprob};
+  for (const void* w : words) if (!aligned(w, 4)) return VS_ERR_INVALID_ARG;
+  OnDevice on(x->device);
   if (!on.ok) return VS_ERR_CUDA;
-  ScoreArgs a = {logits, tokens, logprob, entropy, top_logprob, rank, top_index, row_stride, rows, vocab, top, 1};
+  ScoreArgs a = {x->logits, x->tokens, x->logprob, x->entropy, x->top_logprob, x->rank, x->top_index, x->row_stride, x->rows, x->vocab, x->top, 1};
   // CTAs of a row: as many as leave none of the first 296 places (two an SM) waiting, no more than give a thread something to read
-  const int vectors = (int)((vocab + 16 / el - 1) / (16 / el));
-  while (a.cluster < kMaxCluster && 2 * a.cluster * rows <= 296 && vectors > 2 * a.cluster * kThreads) a.cluster *= 2;
-  const bool vector = aligned(logits, 16) && (row_stride * (int64_t)el) % 16 == 0;
+  const int vectors = (int)((x->vocab + 16 / el - 1) / (16 / el));
+  while (a.cluster < kMaxCluster && 2ll * a.cluster * x->rows <= 296 && vectors > 2 * a.cluster * kThreads) a.cluster *= 2;
+  const bool vector = aligned(x->logits, 16) && (x->row_stride * (int64_t)el) % 16 == 0;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  if (dtype == 1) return vector ? launch<float, true>(a, st) : launch<float, false>(a, st);
+  if (x->dtype == 1) return vector ? launch<float, true>(a, st) : launch<float, false>(a, st);
   return vector ? launch<bf16, true>(a, st) : launch<bf16, false>(a, st);
 }
