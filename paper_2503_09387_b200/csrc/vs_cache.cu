@@ -103,9 +103,10 @@ __global__ void __launch_bounds__(kThreads) cache_write_kernel(const __grid_cons
       const uint2 w = *at;
       uint32_t q[2] = {0u, 0u};
 #pragma unroll
-      for (int h = 0; h < 4; ++h) {
-        const float2 f = codes_to_float2(((h < 2 ? w.x : w.y) >> (16 * (h & 1))) & 0xffffu);
-        q[h >> 1] |= float2_to_codes(f.x * down, f.y * down) << (16 * (h & 1));
+      for (int h = 0; h < 2; ++h) {
+        float f[4];
+        codes_to_floats(h ? w.y : w.x, f);
+        q[h] = float2_to_codes(f[0] * down, f[1] * down) | float2_to_codes(f[2] * down, f[3] * down) << 16;
       }
       *at = make_uint2(q[0], q[1]);
     }
@@ -146,10 +147,11 @@ __global__ void __launch_bounds__(kThreads) cache_read_kernel(const __grid_const
     if (t >= p.n) continue;
     float x[8];
 #pragma unroll
-    for (int h = 0; h < 4; ++h) {
-      const float2 f = codes_to_float2(((h < 2 ? w[u].x : w[u].y) >> (16 * (h & 1))) & 0xffffu);
-      x[2 * h] = f.x * scale;
-      x[2 * h + 1] = f.y * scale;
+    for (int h = 0; h < 2; ++h) {
+      float f[4];
+      codes_to_floats(h ? w[u].y : w[u].x, f);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[4 * h + e] = f[e] * scale;
     }
     store8(rows + t * step + c * 8, x);
   }

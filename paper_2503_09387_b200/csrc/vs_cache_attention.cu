@@ -11,9 +11,9 @@
 // rounded to fp16 (a half step, 2^-12 relative; the smallest, 2^-40 of the largest, is far below any sum's last bit); maxima, sums and rows are fp32.
 //
 // What bounds the few-row kernel: the codes' bytes, once from HBM.  All heads of a KV group, and a few tokens, are the 8 (or 16)
-// columns of mma.sync: S^T = K q^T and O^T += V^T P^T, 16 keys a step, so a page is read once for the whole group; a tcgen05 tile of 128
-// rows would hold 7.  A CTA is four warps, each with 16 keys of a page in a ring of its own, filled by 16-byte asynchronous copies
-// kStages - 1 pages ahead and placed so that both operands' fragments are read without bank conflicts: no barrier in the loop.
+// columns of mma.sync: S^T = K q^T and O^T += V^T P^T, so a page is read once for the whole group; a tcgen05 tile of 128
+// rows would hold 7.  A CTA is four warps, each with half a page in a ring of its own, filled by 16-byte asynchronous copies
+// ahead of their turn and placed so that both operands' fragments are read without bank conflicts: no barrier in the loop.
 // The work of all sequences is cut into equal runs of pages (count_units): long and short sequences side by side leave no CTA idle.
 #include "vs_cache_attention.cuh"
 #include "vs_ptx.cuh"
@@ -22,7 +22,7 @@ namespace vs {
 
 namespace {
 
-constexpr int kWarps = 4, kThreads = 32 * kWarps, kWarpKeys = kPage / kWarps, kStages = 4;
+constexpr int kWarps = 4, kThreads = 32 * kWarps, kWarpKeys = 32, kStepPages = kWarps * kWarpKeys / kPage;
 constexpr float kLift = 15.f;
 
 __device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -46,7 +46,7 @@ __device__ __forceinline__ uint2 lds64(uint32_t addr) {
 
 template <int D, int NT>
 struct Few {
-  static constexpr int W = 8 * NT;
+  static constexpr int W = 8 * NT, kStages = D == 128 ? 2 : 4;
   static constexpr int kTile = kWarpKeys * D;                      // a warp's keys (or values) of a page, bytes
   static constexpr int kStage = 2 * kTile;
   static constexpr int kRing = kWarps * kStages * kStage;
@@ -57,7 +57,7 @@ struct Few {
   static int bytes(int n_seqs) { return kBefore + 8 * (n_seqs + 1); }
 };
 
-// Places of a 16-byte piece c of row r (0..15): keys are read by quads of lanes, eight rows side by side; values by eight lanes of one
+// Places of a 16-byte piece c of row r: keys are read by quads of lanes, eight rows side by side; values by eight lanes of one
 // piece each, rows 2 q apart.  The exclusive or spreads either over all banks.
 __device__ __forceinline__ uint32_t k_place(int r, int c, int D) { return (uint32_t)(r * D + ((D == 128 ? c ^ ((r & 1) << 2) : c) << 4)); }
 __device__ __forceinline__ uint32_t v_place(int r, int c, int D) { return (uint32_t)(r * D + ((D == 128 ? c ^ (r & 6) : c) << 4)); }
@@ -75,8 +75,8 @@ __global__ void __launch_bounds__(kThreads) cache_attention_few_kernel(const __g
   if (tid == 0) a.joins[cta] = make_int4(0, 0, 0, 0);
   if (cta >= n_ctas || units == 0) return;
   const long long u_begin = run_begin(units, n_ctas, cta), u_end = run_begin(units, n_ctas, cta + 1);
-  const uint32_t ring = smem_u32(smem) + (uint32_t)(warp * kStages * F::kStage);
-  float2* meta = reinterpret_cast<float2*>(smem + F::kMeta) + warp * kStages;
+  const uint32_t ring = smem_u32(smem) + (uint32_t)(warp * F::kStages * F::kStage);
+  float2* meta = reinterpret_cast<float2*>(smem + F::kMeta) + warp * F::kStages;
 
   for (long long u = u_begin; u < u_end;) {
     const AttnItem it = item_at<W>(a, before, u, u_end);
@@ -85,28 +85,34 @@ __global__ void __launch_bounds__(kThreads) cache_attention_few_kernel(const __g
     u += it.n;
     const int r0 = it.tile * W, n_cols = (int)min((long long)W, (long long)s.n * a.G - r0);
 
-    // ---- pages on their way ---------------------------------------------------------------------------------
-    auto load_page = [&](int i) {
-      if (i < it.n) {
-        const int page = page_of(a.r, a.c.n_pages, it.seq, it.page + i);
-        const size_t tile = (size_t)max(page, 0) * a.c.n_kv_heads + it.head;
-        const uint8_t* k = static_cast<const uint8_t*>(a.c.k) + tile * (kPage * D) + warp * F::kTile;
-        const uint8_t* v = static_cast<const uint8_t*>(a.c.v) + tile * (kPage * D) + warp * F::kTile;
-        const uint32_t at = ring + (uint32_t)((i % kStages) * F::kStage);
+    // ---- pages on their way: step i of the item, the warp's half of one of its two pages ----------------------------
+    int id = -1;                     // page (of the 32 that the step being loaded is among) lane `lane`, and its scales
+    float2 sc_mine = make_float2(-1.f, 1.f);
+    auto load_step = [&](int i) {
+      if (kStepPages * i < it.n) {
+        const int p = kStepPages * i + warp / 2;
+        if (((kStepPages * i) & 31) == 0) {
+          id = kStepPages * i + lane < it.n ? page_of(a.r, a.c.n_pages, it.seq, it.page + kStepPages * i + lane) : -1;
+          const size_t at = (size_t)max(id, 0) * a.c.n_kv_heads + it.head;
+          sc_mine = id >= 0 ? make_float2(a.c.k_scale[at], a.c.v_scale[at]) : make_float2(-1.f, 1.f);       // (no page has a negative scale)
+        }
+        const int page = __shfl_sync(0xffffffffu, id, p & 31);
+        const size_t from = ((size_t)max(page, 0) * a.c.n_kv_heads + it.head) * (size_t)(kPage * D) + (size_t)((warp & 1) * F::kTile + lane * 16);
+        const uint8_t *k = static_cast<const uint8_t*>(a.c.k) + from, *v = static_cast<const uint8_t*>(a.c.v) + from;
+        const uint32_t at = ring + (uint32_t)((i % F::kStages) * F::kStage);
 #pragma unroll
         for (int j = 0; j < F::kTile / 512; ++j) {
-          const int p = j * 32 + lane, r = p / CPR, c = p % CPR;
-          cp_async16(at + k_place(r, c, D), k + p * 16, page >= 0);
-          cp_async16(at + (uint32_t)F::kTile + v_place(r, c, D), v + p * 16, page >= 0);
+          const int r = (j * 32 + lane) / CPR, c = lane % CPR;
+          cp_async16(at + k_place(r, c, D), k + j * 512, page >= 0);
+          cp_async16(at + (uint32_t)F::kTile + v_place(r, c, D), v + j * 512, page >= 0);
         }
-        // (a page that is not there: a negative scale, which no page has)
-        if (lane == 0) meta[i % kStages] = page >= 0 ? make_float2(a.c.k_scale[tile], a.c.v_scale[tile]) : make_float2(-1.f, 1.f);
+        if (lane == (p & 31)) meta[i % F::kStages] = sc_mine;
       }
       cp_async_commit();
     };
     __syncthreads();                 // the rows of the item before, in the ring, have been read
 #pragma unroll
-    for (int i = 0; i < kStages - 1; ++i) load_page(i);
+    for (int i = 0; i < F::kStages - 1; ++i) load_step(i);
 
     // ---- the query: column n of a B operand, 16 (q4 + 4 i) + 4 w + e of the row in k-step 4 i + w --------------------
     uint32_t qf[NT][KS][2];
@@ -173,48 +179,54 @@ __global__ void __launch_bounds__(kThreads) cache_attention_few_kernel(const __g
       l_run[n][0] = l_run[n][1] = 0.f;
     }
 
-    for (int i = 0; i < it.n; ++i) {
-      cp_async_wait<kStages - 2>();
-      __syncwarp();                  // this page is here, and every lane is done with the one before
-      load_page(i + kStages - 1);
-      const uint32_t at = ring + (uint32_t)((i % kStages) * F::kStage);
-      const float2 scales = meta[i % kStages];
-      const int key0 = (it.page + i) * kPage + warp * kWarpKeys;
-      const bool there = scales.x >= 0.f;
-      if (!there || key0 >= any_hi || key0 + kWarpKeys <= any_lo) continue;      // (the same for the whole warp)
-      // S^T = K q^T
-      float sc[NT][4];
+    for (int i = 0; kStepPages * i < it.n; ++i) {
+      __syncwarp();                  // every lane is done with the step before: its place in the ring is free
+      load_step(i + F::kStages - 1);
+      cp_async_wait<F::kStages - 1>();
+      __syncwarp();                  // this step's codes are here
+      const uint32_t at = ring + (uint32_t)((i % F::kStages) * F::kStage);
+      const bool mine = kStepPages * i + warp / 2 < it.n;
+      const float2 scales = mine ? meta[i % F::kStages] : make_float2(-1.f, 1.f);
+      const int key0 = (it.page + kStepPages * i + warp / 2) * kPage + (warp & 1) * kWarpKeys;
+      if (scales.x < 0.f || key0 >= any_hi || key0 + kWarpKeys <= any_lo) continue;      // (the same for the whole warp)
+      // S^T = K q^T, two tiles of 16 keys
+      float sc[NT][2][4];
 #pragma unroll
-      for (int n = 0; n < NT; ++n) sc[n][0] = sc[n][1] = sc[n][2] = sc[n][3] = 0.f;
+      for (int n = 0; n < NT; ++n)
 #pragma unroll
-      for (int h = 0; h < KS / 4; ++h) {
-        const uint4 ka = lds128(at + k_place(g, q4 + 4 * h, D)), kb = lds128(at + k_place(g + 8, q4 + 4 * h, D));
+        for (int b = 0; b < 2; ++b) sc[n][b][0] = sc[n][b][1] = sc[n][b][2] = sc[n][b][3] = 0.f;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          const uint32_t x = word(ka, w), y = word(kb, w);
-          const uint32_t a0 = codes_to_half2(x & 0xffffu), a2 = codes_to_half2(x >> 16), a1 = codes_to_half2(y & 0xffffu), a3 = codes_to_half2(y >> 16);
+      for (int b = 0; b < 2; ++b)
 #pragma unroll
-          for (int n = 0; n < NT; ++n) mma_f16(sc[n], a0, a1, a2, a3, qf[n][4 * h + w][0], qf[n][4 * h + w][1]);
+        for (int h = 0; h < KS / 4; ++h) {
+          const uint4 ka = lds128(at + k_place(16 * b + g, q4 + 4 * h, D)), kb = lds128(at + k_place(16 * b + g + 8, q4 + 4 * h, D));
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            uint32_t a0, a1, a2, a3;
+            codes_to_half2(word(ka, w), a0, a2);
+            codes_to_half2(word(kb, w), a1, a3);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) mma_f16(sc[n][b], a0, a1, a2, a3, qf[n][4 * h + w][0], qf[n][4 * h + w][1]);
+          }
         }
-      }
       const int ev = exponent_of(scales.y);
       const float evf = (float)ev, down = power_of_two(-ev);
       const bool edge = key0 < all_lo || key0 + kWarpKeys > all_hi;
-      uint32_t pf[NT][2];
+      uint32_t pf[NT][2][2];
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
-        float x[4], mx[2] = {-INFINITY, -INFINITY};
+        // x of keys g + 8 k of columns 2 q4, 2 q4 + 1: x[2 k], x[2 k + 1]
+        float x[8], mx[2], m_new[2];
+        bool moved = false, far[2];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          x[j] = fmaf(sc[n][j], factor[n][j & 1] * scales.x, evf);
+        for (int j = 0; j < 8; ++j) {
+          x[j] = fmaf(sc[n][j >> 2][j & 3], factor[n][j & 1] * scales.x, evf);
           const int key = key0 + g + 8 * (j >> 1);
           if (edge && (key >= hi_of[n][j & 1] || key < lo_of[n][j & 1])) x[j] = -INFINITY;
-          mx[j & 1] = fmaxf(mx[j & 1], x[j]);
         }
-        bool moved = false, far[2];
-        float m_new[2];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
+          mx[j] = fmaxf(fmaxf(x[j], x[j + 2]), fmaxf(x[j + 4], x[j + 6]));
           mx[j] = fmaxf(mx[j], __shfl_xor_sync(0xffffffffu, mx[j], 4));
           mx[j] = fmaxf(mx[j], __shfl_xor_sync(0xffffffffu, mx[j], 8));
           mx[j] = fmaxf(mx[j], __shfl_xor_sync(0xffffffffu, mx[j], 16));
@@ -236,53 +248,59 @@ __global__ void __launch_bounds__(kThreads) cache_attention_few_kernel(const __g
 #pragma unroll
             for (int j = 0; j < 4; ++j) o[n][i2][j] *= r[j & 1];
         }
-        float p[4];
+        const float ref[2] = {m_run[n][0] == -INFINITY ? 0.f : m_run[n][0] - kLift, m_run[n][1] == -INFINITY ? 0.f : m_run[n][1] - kLift};
+        float p[8];
         if (!__any_sync(0xffffffffu, far[0] || far[1])) {
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            p[j] = ex2_approx(x[j] - (m_run[n][j & 1] == -INFINITY ? 0.f : m_run[n][j & 1] - kLift));
-            l_run[n][j & 1] = fmaf(p[j], down, l_run[n][j & 1]);
-          }
+          for (int j = 0; j < 8; ++j) p[j] = ex2_approx(x[j] - ref[j & 1]);
+#pragma unroll
+          for (int j = 0; j < 2; ++j) l_run[n][j] = fmaf((p[j] + p[j + 2]) + (p[j + 4] + p[j + 6]), down, l_run[n][j]);
         } else {
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
+          for (int j = 0; j < 8; ++j) {
             const int c = j & 1;
-            const float ref = far[c] ? mx[c] : (m_run[n][c] == -INFINITY ? 0.f : m_run[n][c] - kLift);
-            p[j] = ex2_approx(x[j] - ref);
-            l_run[n][c] = fmaf(p[j], far[c] ? exp2f(mx[c] - m_run[n][c] + kLift - evf) : down, l_run[n][c]);
+            p[j] = ex2_approx(x[j] - (far[c] ? mx[c] : ref[c]));
+            l_run[n][c] = fmaf(p[j], far[c] ? exp2f(mx[c] - ref[c] - evf) : down, l_run[n][c]);
             if (far[c]) p[j] = 0.f;
           }
         }
-        pf[n][0] = transpose_8x8(half2_of(p[0], p[1]));
-        pf[n][1] = transpose_8x8(half2_of(p[2], p[3]));
-      }
-      // O^T += V^T P^T: the lane's piece of dims, keys 2 q4, 2 q4 + 1, 2 q4 + 8, 2 q4 + 9
-      uint32_t vw[4][D / 32];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int r = 2 * q4 + (j & 1) + 8 * (j >> 1);
-        if constexpr (D == 128) {
-          const uint4 v = lds128(at + (uint32_t)F::kTile + v_place(r, g, D));
-          vw[j][0] = v.x; vw[j][1] = v.y; vw[j][2] = v.z; vw[j][3] = v.w;
-        } else {
-          const uint2 v = lds64(at + (uint32_t)F::kTile + v_place(r, g >> 1, D) + 8u * (uint32_t)(g & 1));
-          vw[j][0] = v.x; vw[j][1] = v.y;
+        for (int b = 0; b < 2; ++b) {
+          pf[n][b][0] = transpose_8x8(half2_of(p[4 * b], p[4 * b + 1]));
+          pf[n][b][1] = transpose_8x8(half2_of(p[4 * b + 2], p[4 * b + 3]));
         }
-        // what no row sees may be anything, NaN among it, which a weight of 0 does not stop
-        if (edge && (key0 + r >= any_hi || key0 + r < any_lo))
-#pragma unroll
-          for (int w = 0; w < D / 32; ++w) vw[j][w] = 0u;
       }
+      // O^T += V^T P^T: the lane's piece of dims, keys 2 q4, 2 q4 + 1, 2 q4 + 8, 2 q4 + 9 of either tile
 #pragma unroll
-      for (int w = 0; w < D / 32; ++w)
+      for (int b = 0; b < 2; ++b) {
+        uint32_t vw[4][D / 32];
 #pragma unroll
-        for (int hh = 0; hh < 2; ++hh) {
-          // bytes 2 hh and 2 hh + 1 of the four keys' words
-          const uint32_t x = __byte_perm(vw[0][w], vw[1][w], hh ? 0x7362 : 0x5140), y = __byte_perm(vw[2][w], vw[3][w], hh ? 0x7362 : 0x5140);
-          const uint32_t a0 = codes_to_half2(x & 0xffffu), a1 = codes_to_half2(x >> 16), a2 = codes_to_half2(y & 0xffffu), a3 = codes_to_half2(y >> 16);
+        for (int j = 0; j < 4; ++j) {
+          const int r = 16 * b + 2 * q4 + (j & 1) + 8 * (j >> 1);
+          if constexpr (D == 128) {
+            const uint4 v = lds128(at + (uint32_t)F::kTile + v_place(r, g, D));
+            vw[j][0] = v.x; vw[j][1] = v.y; vw[j][2] = v.z; vw[j][3] = v.w;
+          } else {
+            const uint2 v = lds64(at + (uint32_t)F::kTile + v_place(r, g >> 1, D) + 8u * (uint32_t)(g & 1));
+            vw[j][0] = v.x; vw[j][1] = v.y;
+          }
+          // what no row sees may be anything, NaN among it, which a weight of 0 does not stop
+          if (edge && (key0 + r >= any_hi || key0 + r < any_lo))
 #pragma unroll
-          for (int n = 0; n < NT; ++n) mma_f16(o[n][2 * w + hh], a0, a1, a2, a3, pf[n][0], pf[n][1]);
+            for (int w = 0; w < D / 32; ++w) vw[j][w] = 0u;
         }
+#pragma unroll
+        for (int w = 0; w < D / 32; ++w)
+#pragma unroll
+          for (int hh = 0; hh < 2; ++hh) {
+            // bytes 2 hh and 2 hh + 1 of the four keys' words
+            uint32_t a0, a1, a2, a3;
+            codes_to_half2(__byte_perm(vw[0][w], vw[1][w], hh ? 0x7362 : 0x5140), a0, a1);
+            codes_to_half2(__byte_perm(vw[2][w], vw[3][w], hh ? 0x7362 : 0x5140), a2, a3);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) mma_f16(o[n][2 * w + hh], a0, a1, a2, a3, pf[n][b][0], pf[n][b][1]);
+          }
+      }
     }
     cp_async_wait<0>();
     __syncthreads();                 // nobody reads the ring any more

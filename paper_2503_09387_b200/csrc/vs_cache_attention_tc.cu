@@ -290,8 +290,13 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attention_tc_kernel(const _
           for (int i = 0; i < PER; ++i) {
             const int r = h * kPage + row[i], c = 2 * (piece[i] & 3);
             const uint32_t at = to + (uint32_t)((piece[i] >> 2) * (kStepKeys * 128) + r * 128);
-            sts128(at + (uint32_t)((c ^ (r & 7)) << 4), codes_to_half2(v[i].x & 0xffffu), codes_to_half2(v[i].x >> 16), codes_to_half2(v[i].y & 0xffffu), codes_to_half2(v[i].y >> 16));
-            sts128(at + (uint32_t)(((c + 1) ^ (r & 7)) << 4), codes_to_half2(v[i].z & 0xffffu), codes_to_half2(v[i].z >> 16), codes_to_half2(v[i].w & 0xffffu), codes_to_half2(v[i].w >> 16));
+            uint32_t x[8];
+            codes_to_half2(v[i].x, x[0], x[1]);
+            codes_to_half2(v[i].y, x[2], x[3]);
+            codes_to_half2(v[i].z, x[4], x[5]);
+            codes_to_half2(v[i].w, x[6], x[7]);
+            sts128(at + (uint32_t)((c ^ (r & 7)) << 4), x[0], x[1], x[2], x[3]);
+            sts128(at + (uint32_t)(((c + 1) ^ (r & 7)) << 4), x[4], x[5], x[6], x[7]);
           }
           ++raw;
         }

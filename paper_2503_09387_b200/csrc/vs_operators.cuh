@@ -60,15 +60,15 @@ __device__ __forceinline__ int page_of(const vs_cache_seqs& r, int n_pages, int 
 __device__ __forceinline__ int exponent_of(float scale) { return (int)((__float_as_uint(scale) >> 23) & 255u) - 127; }
 __device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)min(max(e + 127, 0), 254) << 23); }   // (0 below 2^-126)
 
-// two e4m3 codes (low byte first) <-> two values
-__device__ __forceinline__ uint32_t codes_to_half2(uint32_t two) {
-  uint32_t r;
-  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"((unsigned short)two));
-  return r;
+// e4m3 codes (low byte first) -> values
+__device__ __forceinline__ void codes_to_half2(uint32_t four, uint32_t& low, uint32_t& high) {
+  asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, l;\n\tcvt.rn.f16x2.e4m3x2 %1, h;\n\t}" : "=r"(low), "=r"(high) : "r"(four));
 }
-__device__ __forceinline__ float2 codes_to_float2(uint32_t two) {
-  const uint32_t h = codes_to_half2(two);
-  return __half22float2(*reinterpret_cast<const __half2*>(&h));
+__device__ __forceinline__ void codes_to_floats(uint32_t four, float (&x)[4]) {
+  uint32_t l, h;
+  codes_to_half2(four, l, h);
+  const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&l)), b = __half22float2(*reinterpret_cast<const __half2*>(&h));
+  x[0] = a.x; x[1] = a.y; x[2] = b.x; x[3] = b.y;
 }
 // nearest code, ties to the even one, magnitudes above 448 to 448, NaN to NaN
 __device__ __forceinline__ uint32_t float2_to_codes(float lo, float hi) {
