@@ -71,19 +71,20 @@ __global__ void __launch_bounds__(kThreads) cache_attention_few_kernel(const __g
   long long* before = reinterpret_cast<long long*>(smem + F::kBefore);
   pdl_launch_dependents();
   const long long units = count_units<W>(a, before);
-  const int n_ctas = ctas_at_work(a, units, (int)gridDim.x), cta = (int)blockIdx.x;
+  const AttnRuns runs(a, units, (int)gridDim.x);
+  const int cta = (int)blockIdx.x;
   if (tid == 0) a.joins[cta] = make_int4(0, 0, 0, 0);
-  if (cta >= n_ctas || units == 0) return;
-  const long long u_begin = run_begin(units, n_ctas, cta), u_end = run_begin(units, n_ctas, cta + 1);
+  if (cta >= runs.n_ctas || units == 0) return;
+  const long long u_begin = runs.begin(cta), u_end = runs.begin(cta + 1);
   const uint32_t ring = smem_u32(smem) + (uint32_t)(warp * F::kStages * F::kStage);
   float2* meta = reinterpret_cast<float2*>(smem + F::kMeta) + warp * F::kStages;
 
   for (long long u = u_begin; u < u_end;) {
     const AttnItem it = item_at<W>(a, before, u, u_end);
-    if (it.n < 1) break;             // (only if the sequences changed under the kernel)
-    const SeqShape s = shape_of<W>(a, it.seq);
+    if (it.n < 1) break;
+    const SeqShape& s = it.s;
+    const int r0 = it.r0, n_cols = it.n_cols;
     u += it.n;
-    const int r0 = it.tile * W, n_cols = (int)min((long long)W, (long long)s.n * a.G - r0);
 
     // ---- pages on their way: step i of the item, the warp's half of one of its two pages ----------------------------
     int id = -1;                     // page (of the 32 that the step being loaded is among) lane `lane`, and its scales
@@ -120,8 +121,8 @@ __global__ void __launch_bounds__(kThreads) cache_attention_few_kernel(const __g
     int hi_of[NT][2], lo_of[NT][2];  // keys that they see
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-      const int col = 8 * n + g, r = r0 + min(col, n_cols - 1), t = r / a.G, h = it.head * a.G + (r - t * a.G);
-      const bf16* row = a.q + (long long)(s.first + t) * a.q_row + (long long)h * a.q_head;
+      const int col = 8 * n + g, r = r0 + min(col, n_cols - 1), t = by_group(a, r);
+      const bf16* row = a.q + (long long)(s.first + t) * a.q_row + (long long)(it.head * a.G + (r - t * a.G)) * a.q_head;
       uint4 raw[KS / 4][2];
       float amax = 0.f;
 #pragma unroll
@@ -346,115 +347,119 @@ __global__ void __launch_bounds__(kThreads) cache_attention_few_kernel(const __g
         if (d == 0) part_stats<W, D>(a.parts, cta, begun ? 0 : 1)[col] = make_float2(m - kLift, l);
       } else {
         const float inv = l == 0.f ? 0.f : 1.f / l;
-        store_row_piece(a, s.first, r0 + col, it.head, d, make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv));
-        if (d == 0) store_lse(a, s.first, r0 + col, it.head, m - kLift, l);
+        const RowHead to = row_head(a, s.first, r0 + col, it.head);
+        store_row_piece(a, to, d, make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv));
+        if (d == 0) store_lse(a, to, m - kLift, l);
       }
     }
     if (begun && !goes_on && tid == 0) {
-      const long long u_item = u - it.of;                          // the item's first unit
-      a.joins[cta] = make_int4(1 + cta_of(units, n_ctas, u_item), s.first, r0, it.head | (n_cols << 16));
+      a.joins[cta] = make_int4(1 + runs.cta_of(u - it.of), s.first, r0, it.head | (n_cols << 16));
     }
   }
 }
 
 // ---- rows that several CTAs worked on ------------------------------------------------------------------------------
-// A block lists the CTAs that were the last on an item others had begun, then takes columns of those items by turns: kCols at a time, the
-// parts of each shared by 8 / kCols warps, a lane four dims.
-constexpr int kJoinThreads = 256, kJoinBlocks = 4 * 148;
-template <int W, int D, int kCols>
-__global__ void __launch_bounds__(kJoinThreads) cache_attention_join_kernel(const __grid_constant__ CacheAttnArgs a, int ctas) {
-  constexpr int WPC = 8 / kCols, GROUPS = W / kCols, U = 4;
-  constexpr int CHUNKS = (kFewCtas + 31) / 32;
-  __shared__ int list[kFewCtas], count[CHUNKS];
-  __shared__ float2 sm_st[8];
-  __shared__ float4 sm_o[8][D / 4];
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  pdl_wait();
+constexpr int kJoinWarps = 8, kJoinThreads = 32 * kJoinWarps, kJoinBlocks = 4 * 148;
+struct JoinShared {
+  int list[kFewCtas], count[(kFewCtas + 31) / 32];
+  float2 st[kJoinWarps];
+  float4 o[kJoinWarps][32];
+};
+// A part of a row: a lane four dims of it
+struct Sum { float m, l; float4 o; };
+__device__ __forceinline__ void add_part(Sum& s, float2 st, float4 v) {
+  if (st.x == -INFINITY) return;
+  const float m = fmaxf(s.m, st.x), fa = s.m == -INFINITY ? 0.f : exp2f(s.m - m), fb = exp2f(st.x - m);
+  s.o.x = s.o.x * fa + v.x * fb; s.o.y = s.o.y * fa + v.y * fb; s.o.z = s.o.z * fa + v.z * fb; s.o.w = s.o.w * fa + v.w * fb;
+  s.l = (s.m == -INFINITY ? 0.f : times_power(s.l, s.m - m)) + times_power(st.y, st.x - m);
+  s.m = m;
+}
+// The items that a kernel's CTAs left in parts, by all blocks: a block lists the CTAs that were the last on an item others had begun.  Where
+// these are many it takes eight columns of an item at a time, a warp to each; else one, its parts shared by the warps.
+template <int W, int D>
+__device__ __forceinline__ void join_items(const CacheAttnArgs& a, const int4* joins, float* parts, int ctas, JoinShared& sm) {
+  constexpr int CHUNKS = (kFewCtas + 31) / 32, PER = (CHUNKS + kJoinWarps - 1) / kJoinWarps;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   // (in the order of the CTAs: the same list in every block)
-  unsigned set[(CHUNKS + 7) / 8];
+  unsigned set[PER];
 #pragma unroll
-  for (int k = 0; k < (CHUNKS + 7) / 8; ++k) {
-    const int chunk = warp + 8 * k, c = 32 * chunk + lane;
-    set[k] = __ballot_sync(0xffffffffu, c < ctas && a.joins[min(c, ctas - 1)].x != 0);
-    if (lane == 0 && chunk < CHUNKS) count[chunk] = __popc(set[k]);
+  for (int k = 0; k < PER; ++k) {
+    const int chunk = warp + kJoinWarps * k, c = 32 * chunk + lane;
+    set[k] = __ballot_sync(0xffffffffu, c < ctas && joins[min(c, ctas - 1)].x != 0);
+    if (lane == 0 && chunk < CHUNKS) sm.count[chunk] = __popc(set[k]);
   }
   __syncthreads();
   int listed = 0;
-  for (int i = 0; i < CHUNKS; ++i) listed += count[i];
+  for (int i = 0; i < CHUNKS; ++i) listed += sm.count[i];
 #pragma unroll
-  for (int k = 0; k < (CHUNKS + 7) / 8; ++k) {
-    const int chunk = warp + 8 * k;
+  for (int k = 0; k < PER; ++k) {
+    const int chunk = warp + kJoinWarps * k;
     int at = __popc(set[k] & ((1u << lane) - 1u));
-    for (int i = 0; i < min(chunk, CHUNKS); ++i) at += count[i];
-    if ((set[k] >> lane) & 1u) list[at] = 32 * chunk + lane;
+    for (int i = 0; i < min(chunk, CHUNKS); ++i) at += sm.count[i];
+    if ((set[k] >> lane) & 1u) sm.list[at] = 32 * chunk + lane;
   }
   __syncthreads();
-  const int n = listed * GROUPS;
-  for (int at = (int)blockIdx.x; at < n; at += (int)gridDim.x) {
-    const int last = list[at / GROUPS], col = (at % GROUPS) * kCols + warp / WPC, share = warp % WPC;
-    const int4 j = a.joins[last];
+  const bool wide = W >= 8 * kJoinWarps && listed * (W / kJoinWarps) >= (int)gridDim.x;
+  const int groups = wide ? W / kJoinWarps : W, step = wide ? 1 : kJoinWarps;
+  for (int at = (int)blockIdx.x; at < listed * groups; at += (int)gridDim.x) {
+    const int last = sm.list[at / groups], col = wide ? (at % groups) * kJoinWarps + warp : at % groups;
+    const int4 j = joins[last];
     const int first = j.x - 1;
-    const bool on = col < (j.w >> 16);
-    float m = -INFINITY, l = 0.f;
-    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int c0 = first + share; c0 <= last && on; c0 += U * WPC) {
+    const bool on = col < (j.w >> 16);                      // (the whole warp; without `wide` the whole block)
+    Sum s = {-INFINITY, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
+    constexpr int U = 4;
+    for (int c0 = first + (wide ? 0 : warp); c0 <= last && on; c0 += U * step) {
       float2 st[U];
       float4 v[U];
 #pragma unroll
       for (int i = 0; i < U; ++i) {
-        const int c = c0 + i * WPC;
+        const int c = c0 + i * step, place = c == first ? 1 : 0;
         st[i] = make_float2(-INFINITY, 0.f);
         v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
         if (c <= last) {
-          const int place = c == first ? 1 : 0;
-          st[i] = part_stats<W, D>(a.parts, c, place)[col];
-          if (lane < D / 4) v[i] = *reinterpret_cast<const float4*>(part_rows<W, D>(a.parts, c, place) + (size_t)col * D + 4 * lane);
+          st[i] = part_stats<W, D>(parts, c, place)[col];
+          if (lane < D / 4) v[i] = *reinterpret_cast<const float4*>(part_rows<W, D>(parts, c, place) + (size_t)col * D + 4 * lane);
         }
       }
 #pragma unroll
-      for (int i = 0; i < U; ++i) {
-        if (st[i].x == -INFINITY) continue;
-        const float m_new = fmaxf(m, st[i].x), fa = m == -INFINITY ? 0.f : exp2f(m - m_new), fb = exp2f(st[i].x - m_new);
-        o.x = o.x * fa + v[i].x * fb; o.y = o.y * fa + v[i].y * fb; o.z = o.z * fa + v[i].z * fb; o.w = o.w * fa + v[i].w * fb;
-        l = (m == -INFINITY ? 0.f : times_power(l, m - m_new)) + times_power(st[i].y, st[i].x - m_new);
-        m = m_new;
-      }
+      for (int i = 0; i < U; ++i) add_part(s, st[i], v[i]);
     }
-    if (lane == 0) sm_st[warp] = make_float2(m, l);
-    if (lane < D / 4) sm_o[warp][lane] = o;
-    __syncthreads();
-    if (on && share == 0 && lane < D / 4) {
-      float M = -INFINITY, sum = 0.f;
-#pragma unroll
-      for (int w = 0; w < WPC; ++w) M = fmaxf(M, sm_st[warp + w].x);
-      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-      for (int w = 0; w < WPC; ++w) {
-        const float2 st = sm_st[warp + w];
-        const float f = st.x == -INFINITY ? 0.f : exp2f(st.x - M);
-        const float4 x = sm_o[warp + w][lane];
-        v.x += f * x.x; v.y += f * x.y; v.z += f * x.z; v.w += f * x.w;
-        sum += st.x == -INFINITY ? 0.f : times_power(st.y, st.x - M);
-      }
-      const float inv = sum == 0.f ? 0.f : 1.f / sum;
-      store_row_piece(a, j.y, j.z + col, j.w & 0xffff, 4 * lane, make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv));
-      if (lane == 0) store_lse(a, j.y, j.z + col, j.w & 0xffff, M, sum);
+    if (!wide) {
+      __syncthreads();                                      // (the round before has been read)
+      if (lane == 0) sm.st[warp] = make_float2(s.m, s.l);
+      sm.o[warp][lane] = s.o;
+      __syncthreads();
+      if (warp != 0) continue;
+      for (int w = 1; w < kJoinWarps; ++w) add_part(s, sm.st[w], sm.o[w][lane]);
     }
-    __syncthreads();
+    if (!on) continue;
+    const float inv = s.l == 0.f ? 0.f : 1.f / s.l;
+    const RowHead to = row_head(a, j.y, j.z + col, j.w & 0xffff);
+    if (lane < D / 4) store_row_piece(a, to, 4 * lane, make_float4(s.o.x * inv, s.o.y * inv, s.o.z * inv, s.o.w * inv));
+    if (lane == 0) store_lse(a, to, s.m, s.l);
   }
+}
+struct Parts { int4* joins; float* parts; };
+template <int D, int WF, bool kMany>
+__global__ void __launch_bounds__(kJoinThreads) cache_attention_join_kernel(const __grid_constant__ CacheAttnArgs a, Parts few, Parts many) {
+  __shared__ JoinShared sm;
+  pdl_wait();
+  if constexpr (WF > 0) join_items<WF, D>(a, few.joins, few.parts, kFewCtas, sm);
+  if constexpr (WF > 0 && kMany) __syncthreads();
+  if constexpr (kMany) join_items<kManyWide, D>(a, many.joins, many.parts, kManyCtas, sm);
 }
 
 template <int D, int NT>
-int launch_few(const CacheAttnArgs& a, int ctas, cudaStream_t st) {
+int launch_few(const CacheAttnArgs& a, cudaStream_t st) {
   using F = Few<D, NT>;
   const int bytes = F::bytes(a.r.n_seqs);
   if (cudaFuncSetAttribute(cache_attention_few_kernel<D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return VS_ERR_CUDA;
-  cache_attention_few_kernel<D, NT><<<ctas, kThreads, bytes, st>>>(a);
+  cache_attention_few_kernel<D, NT><<<kFewCtas, kThreads, bytes, st>>>(a);
   return launched();
 }
 
-template <int W, int D, int kCols>
-int launch_join(const CacheAttnArgs& a, int ctas, cudaStream_t st) {
+template <int D, int WF, bool kMany>
+int launch_join(const CacheAttnArgs& a, Parts few, Parts many, cudaStream_t st) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(kJoinBlocks);
   cfg.blockDim = dim3(kJoinThreads);
@@ -464,35 +469,37 @@ int launch_join(const CacheAttnArgs& a, int ctas, cudaStream_t st) {
   at.val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = &at;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, cache_attention_join_kernel<W, D, kCols>, a, ctas) == cudaSuccess ? launched() : VS_ERR_CUDA;
+  return cudaLaunchKernelEx(&cfg, cache_attention_join_kernel<D, WF, kMany>, a, few, many) == cudaSuccess ? launched() : VS_ERR_CUDA;
+}
+template <int D>
+int join(const CacheAttnArgs& a, Parts few, Parts many, int cols, bool with_many, cudaStream_t st) {
+  if (cols == 0) return launch_join<D, 0, true>(a, few, many, st);
+  if (with_many) return launch_join<D, 16, true>(a, few, many, st);
+  return cols <= 8 ? launch_join<D, 8, false>(a, few, many, st) : launch_join<D, 16, false>(a, few, many, st);
 }
 
 }  // namespace
 
-int launch_cache_attention_few(const CacheAttnArgs& a, int cols, int ctas, cudaStream_t st) {
-  if (cols <= 8) return a.c.head_dim == 128 ? launch_few<128, 1>(a, ctas, st) : launch_few<64, 1>(a, ctas, st);
-  return a.c.head_dim == 128 ? launch_few<128, 2>(a, ctas, st) : launch_few<64, 2>(a, ctas, st);
-}
-int launch_cache_attention_join(const CacheAttnArgs& a, int width, int ctas, cudaStream_t st) {
-  if (width == 8) return a.c.head_dim == 128 ? launch_join<8, 128, 1>(a, ctas, st) : launch_join<8, 64, 1>(a, ctas, st);
-  if (width == 16) return a.c.head_dim == 128 ? launch_join<16, 128, 1>(a, ctas, st) : launch_join<16, 64, 1>(a, ctas, st);
-  return a.c.head_dim == 128 ? launch_join<kManyWide, 128, 4>(a, ctas, st) : launch_join<kManyWide, 64, 4>(a, ctas, st);
+int launch_cache_attention_few(const CacheAttnArgs& a, int cols, cudaStream_t st) {
+  if (cols <= 8) return a.c.head_dim == 128 ? launch_few<128, 1>(a, st) : launch_few<64, 1>(a, st);
+  return a.c.head_dim == 128 ? launch_few<128, 2>(a, st) : launch_few<64, 2>(a, st);
 }
 
 }  // namespace vs
 
 namespace {
-constexpr int kFewMinPages = 4, kManyMinPages = 6;
-// the workspace: status word, the CTAs' notes, their parts
-constexpr size_t kJoinsAt = 256, kPartsAt = 8192;
-static_assert(kJoinsAt + vs::kFewCtas * 16 <= kPartsAt && vs::kManyCtas <= vs::kFewCtas, "notes of the CTAs");
+constexpr int kFewPageShift = 2, kManyPageShift = 2;            // four pages at least
+// the workspace: status word, the CTAs' notes and parts of either kernel
+constexpr size_t kFewJoinsAt = 256, kManyJoinsAt = kFewJoinsAt + vs::kFewCtas * 16, kPartsAt = 16384;
+static_assert(kManyJoinsAt + vs::kManyCtas * 16 <= kPartsAt && vs::kManyCtas <= vs::kFewCtas, "notes of the CTAs");
+size_t few_bytes(int head_dim) { return (size_t)vs::kFewCtas * 2 * vs::kFewCols * (head_dim + 2) * 4; }
+size_t many_bytes(int head_dim) { return (size_t)vs::kManyCtas * 2 * vs::kManyWide * (head_dim + 2) * 4; }
 }
 
 extern "C" int vs_cache_attention_bytes(int32_t head_dim, size_t* out_bytes) {
   if (out_bytes == nullptr) return VS_ERR_INVALID_ARG;
   if (head_dim != 64 && head_dim != 128) return VS_ERR_UNSUPPORTED;
-  const size_t row = (size_t)(head_dim + 2) * 4, few = (size_t)vs::kFewCtas * 2 * vs::kFewCols * row, many = (size_t)vs::kManyCtas * 2 * vs::kManyWide * row;
-  *out_bytes = kPartsAt + (few > many ? few : many);
+  *out_bytes = kPartsAt + few_bytes(head_dim) + many_bytes(head_dim);
   return VS_OK;
 }
 
@@ -518,31 +525,32 @@ extern "C" int vs_cache_attention(const vs_cache* cache, const vs_cache_queries*
   CacheAttnArgs a = {};
   a.c = *cache; a.r = *rows;
   a.q = static_cast<const bf16*>(x->q); a.out = x->out; a.lse = x->lse;
-  a.status = static_cast<int*>(x->workspace);
-  a.joins = reinterpret_cast<int4*>(static_cast<uint8_t*>(x->workspace) + kJoinsAt);
-  a.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(x->workspace) + kPartsAt);
+  uint8_t* ws = static_cast<uint8_t*>(x->workspace);
+  const Parts few = {reinterpret_cast<int4*>(ws + kFewJoinsAt), reinterpret_cast<float*>(ws + kPartsAt)};
+  const Parts many = {reinterpret_cast<int4*>(ws + kManyJoinsAt), reinterpret_cast<float*>(ws + kPartsAt + few_bytes(cache->head_dim))};
+  a.status = reinterpret_cast<int*>(ws);
   a.q_row = x->q_row_stride; a.q_head = x->q_head_stride; a.out_row = x->out_row_stride; a.out_head = x->out_head_stride;
   a.scale_log2e = x->scale * 1.4426950408889634f;
   a.Hq = x->n_q_heads; a.G = G; a.causal = x->causal != 0; a.window = x->window; a.out_fp32 = x->out_dtype;
-  // Which sequences have few rows the device knows; the host, from the number of rows, that all of them have (or none, where they have the
-  // same number each).
+  a.rcp_g = G == 1 ? 0u : (uint32_t)(((1ull << 32) + G - 1) / G);
   const bool uniform = rows->row_offsets == nullptr;
-  const long long most = (uniform ? (long long)(rows->n_rows / rows->n_seqs) : (long long)rows->n_rows) * G;
+  a.rows_each = uniform ? rows->n_rows / rows->n_seqs : -1;
+  a.max_held = rows->table_width >= (1 << 25) ? 0x7fffffff : rows->table_width * kPage;
+  // Which sequences have few rows the device knows; the host, from the number of rows, that all of them have (or none, where they have the
+  // same number each).  Either kind has its kernel; what their CTAs left in parts one launch joins.
+  const long long most = (long long)(uniform ? a.rows_each : rows->n_rows) * G;
+  const bool any_few = most <= kFewCols || !uniform, any_many = most > kFewCols;
+  const int cols = any_few ? (most <= 8 ? 8 : 16) : 0;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  if (most <= kFewCols || !uniform) {
-    a.take_few = 1;
-    a.min_pages = kFewMinPages;
-    const int cols = most <= 8 ? 8 : 16;
-    int r = launch_cache_attention_few(a, cols, kFewCtas, st);
-    if (r == VS_OK) r = launch_cache_attention_join(a, cols, kFewCtas, st);
+  if (any_few) {
+    a.take_few = 1; a.page_shift = kFewPageShift; a.joins = few.joins; a.parts = few.parts;
+    const int r = launch_cache_attention_few(a, cols, st);
     if (r != VS_OK) return r;
   }
-  if (most > kFewCols) {
-    a.take_few = 0;
-    a.min_pages = kManyMinPages;
-    int r = launch_cache_attention_many(a, kManyCtas, st);
-    if (r == VS_OK) r = launch_cache_attention_join(a, kManyWide, kManyCtas, st);
+  if (any_many) {
+    a.take_few = 0; a.page_shift = kManyPageShift; a.joins = many.joins; a.parts = many.parts;
+    const int r = launch_cache_attention_many(a, any_few, st);
     if (r != VS_OK) return r;
   }
-  return VS_OK;
+  return cache->head_dim == 128 ? join<128>(a, few, many, cols, any_many, st) : join<64>(a, few, many, cols, any_many, st);
 }

@@ -1,4 +1,6 @@
 // What the kernels of the attention over a paged cache share: the cut of the work and the parts that a later kernel joins.
+// (A block runs all of this once, from a cold instruction cache, at some 100 clocks for every eight instructions: hence 32-bit numbers, products
+// in the place of divisions, and as little of it as will do.)
 #pragma once
 #include "vs_operators.cuh"
 
@@ -19,44 +21,45 @@ struct CacheAttnArgs {
   long long q_row, q_head, out_row, out_head;
   float scale_log2e;
   int Hq, G, causal, window, out_fp32;
-  int min_pages;                  // pages that are worth a CTA of their own
+  uint32_t rcp_g;                 // 2^32 / G, rounded up (0: G = 1)
+  int rows_each;                  // of every sequence; -1: by row_offsets
+  int max_held;                   // tokens that a sequence's row of the table has pages for
+  int page_shift;                 // log2 of the pages that are worth a CTA of their own
   int take_few;                   // whether the launch takes the sequences of few rows or the others
 };
 
 #ifdef __CUDACC__
+// x / G, x < 2^30
+__device__ __forceinline__ int by_group(const CacheAttnArgs& a, int x) { return a.rcp_g == 0u ? x : (int)__umulhi((uint32_t)x, a.rcp_g); }
+
 // A sequence's packed rows -- row t, head g of the group: t * G + g -- are cut into tiles of W; an item is a tile of one KV head, its work
 // the pages of 64 keys that any of the tile's rows sees (one page at least: an item without keys still has its rows to store).
 struct SeqShape { int first, n, len, tiles; };
 template <int W>
 __device__ __forceinline__ SeqShape shape_of(const CacheAttnArgs& a, int i) {
-  const SeqRows s = rows_of(a.r, i);
-  SeqShape q = {s.first, s.n, max(a.r.tokens[i], 0), 0};
-  const long long cols = (long long)s.n * a.G;
-  if ((cols <= kFewCols) == (a.take_few != 0)) q.tiles = (int)((cols + W - 1) / W);
+  SeqShape q;
+  q.first = a.rows_each * i;
+  q.n = a.rows_each;
+  if (a.rows_each < 0) { const SeqRows s = rows_of(a.r, i); q.first = s.first; q.n = s.n; }
+  q.len = max(a.r.tokens[i], 0);
+  const int cols = q.n * a.G;                       // (the host has seen to it that this is below 2^30)
+  q.tiles = (cols <= kFewCols) == (a.take_few != 0) ? (cols + W - 1) / W : 0;
   return q;
 }
 // keys [lo, hi) that row t of a sequence sees
 struct KeyRange { int lo, hi; };
 __device__ __forceinline__ KeyRange keys_of(const CacheAttnArgs& a, const SeqShape& s, int t) {
-  const long long pos = (long long)s.len - s.n + t;
-  const long long held = min((long long)s.len, (long long)a.r.table_width * kPage);
-  const long long hi = a.causal ? max(min(held, pos + 1), 0ll) : held, lo = a.window > 0 ? max(pos - a.window + 1, 0ll) : 0ll;
-  return {(int)min(lo, hi), (int)hi};
+  const int pos = s.len - s.n + t, held = min(s.len, a.max_held);
+  const int hi = a.causal ? max(min(held, pos + 1), 0) : held;
+  const int lo = a.window > 0 && pos >= a.window ? pos - a.window + 1 : 0;
+  return {min(lo, hi), hi};
 }
 // pages [first, first + n) that tile `tile` sees: those of its first row to those of its last
 struct PageRange { int first, n; };
 template <int W>
 __device__ __forceinline__ PageRange pages_of(const CacheAttnArgs& a, const SeqShape& s, int tile) {
-  const int t0 = (int)((long long)tile * W / a.G), t1 = (int)min(((long long)tile * W + W - 1) / a.G, (long long)s.n - 1);
-  const int lo = keys_of(a, s, t0).lo, hi = keys_of(a, s, t1).hi;
-  const int first = lo / kPage;
-  return {first, max((hi + kPage - 1) / kPage - first, 1)};
-}
-template <int W>
-__device__ __forceinline__ long long units_of(const CacheAttnArgs& a, const SeqShape& s) {
-  long long u = 0;
-  for (int tile = 0; tile < s.tiles; ++tile) u += pages_of<W>(a, s, tile).n;
-  return u * a.c.n_kv_heads;
+  const int first = keys_of(a, s, by_group(a, tile * W)).lo / kPage;
+  return {first, max((keys_of(a, s, min(by_group(a, tile * W + W - 1), s.n - 1)).hi + kPage - 1) / kPage - first, 1)};
 }
 
 // The units (item, page) of all sequences lie end to end and are cut into equal runs, one a CTA.  `before` (shared memory, n_seqs + 1):
@@ -65,43 +68,71 @@ template <int W>
 __device__ __forceinline__ long long count_units(const CacheAttnArgs& a, long long* before) {
   if (threadIdx.x < 32) {
     const int lane = threadIdx.x;
-    long long sum0 = 0;
+    long long ahead = 0;
     for (int base = 0; base < a.r.n_seqs; base += 32) {
       const int i = base + lane;
       long long u = 0;
-      if (i < a.r.n_seqs) u = units_of<W>(a, shape_of<W>(a, i));
+      if (i < a.r.n_seqs) {
+        const SeqShape s = shape_of<W>(a, i);
+#pragma unroll 1
+        for (int tile = 0; tile < s.tiles; ++tile) u += pages_of<W>(a, s, tile).n;
+        u *= a.c.n_kv_heads;
+      }
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) { const long long t = __shfl_up_sync(0xffffffffu, u, o); if (lane >= o) u += t; }
-      if (i < a.r.n_seqs) before[i + 1] = sum0 + u;
-      sum0 += __shfl_sync(0xffffffffu, u, 31);
+      if (i < a.r.n_seqs) before[i + 1] = ahead + u;
+      ahead += __shfl_sync(0xffffffffu, u, 31);
     }
     if (lane == 0) before[0] = 0;
   }
   __syncthreads();
   return before[a.r.n_seqs];
 }
-__device__ __forceinline__ int ctas_at_work(const CacheAttnArgs& a, long long units, int grid) {
-  return (int)max(min((long long)grid, (units + a.min_pages - 1) / a.min_pages), 1ll);
-}
+__device__ __forceinline__ long long divide(long long x, long long y) { return ((x | y) >> 31) == 0 ? (long long)((uint32_t)x / (uint32_t)y) : x / y; }
+// The runs: n_ctas of `each` units, the first `longer` of them of one more.
+struct AttnRuns {
+  long long each;
+  int n_ctas, longer;
+  __device__ __forceinline__ AttnRuns(const CacheAttnArgs& a, long long units, int grid) {
+    n_ctas = (int)min((long long)grid, (units + (1 << a.page_shift) - 1) >> a.page_shift);
+    n_ctas = max(n_ctas, 1);
+    each = divide(units, n_ctas);
+    longer = (int)(units - each * n_ctas);
+  }
+  __device__ __forceinline__ long long begin(int cta) const { return each * cta + min(cta, longer); }
+  // the CTA whose run holds `unit`
+  __device__ __forceinline__ int cta_of(long long unit) const {
+    const long long head = (each + 1) * longer;
+    return unit < head ? (int)divide(unit, each + 1) : longer + (int)divide(unit - head, each);
+  }
+};
 
 // An item's pages that this CTA works on: [page, page + n) of the pages [first, first + of).
-struct AttnItem { int seq, tile, head, page, n, first, of; };
+struct AttnItem { SeqShape s; int seq, r0, n_cols, head, page, n, first, of; };
 template <int W>
 __device__ __forceinline__ AttnItem item_at(const CacheAttnArgs& a, const long long* before, long long unit, long long end) {
-  int lo = 0, hi = a.r.n_seqs - 1;
-  while (lo < hi) { const int mid = (lo + hi + 1) >> 1; if (before[mid] <= unit) lo = mid; else hi = mid - 1; }
-  const SeqShape s = shape_of<W>(a, lo);
+  int lo = 0;
+  if (a.r.n_seqs > 1) {
+    int hi = a.r.n_seqs - 1;
+    while (lo < hi) { const int mid = (lo + hi + 1) >> 1; if (before[mid] <= unit) lo = mid; else hi = mid - 1; }
+  }
+  AttnItem it;
+  it.seq = lo;
+  it.s = shape_of<W>(a, lo);
+  it.n = 0;                           // (stays 0 only if the sequences changed under the kernel)
   long long u = unit - before[lo];
-  AttnItem it = {lo, 0, 0, 0, 0, 0, 0};
-  for (int tile = 0; tile < s.tiles; ++tile) {
-    const PageRange p = pages_of<W>(a, s, tile);
+#pragma unroll 1
+  for (int tile = 0; tile < it.s.tiles; ++tile) {
+    const PageRange p = pages_of<W>(a, it.s, tile);
     const long long here = (long long)p.n * a.c.n_kv_heads;
     if (u < here) {
-      it.tile = tile;
-      it.head = (int)(u / p.n);
-      const int at = (int)(u - (long long)it.head * p.n);
-      it.page = p.first + at;
-      it.n = (int)min((long long)(p.n - at), end - unit);
+      it.r0 = tile * W;
+      it.n_cols = min(W, it.s.n * a.G - it.r0);
+      int head = 0;
+      while (u >= p.n) { u -= p.n; ++head; }
+      it.head = head;
+      it.page = p.first + (int)u;
+      it.n = (int)min((long long)p.n - u, end - unit);
       it.first = p.first;
       it.of = p.n;
       break;
@@ -119,15 +150,6 @@ __device__ __forceinline__ float* part_rows(float* parts, int cta, int place) { 
 template <int W, int D>
 __device__ __forceinline__ float2* part_stats(float* parts, int cta, int place) { return reinterpret_cast<float2*>(part_rows<W, D>(parts, cta, place) + (size_t)W * D); }
 
-__device__ __forceinline__ long long run_begin(long long units, int ctas, int cta) { return units * cta / ctas; }
-// the CTA whose run holds `unit`
-__device__ __forceinline__ int cta_of(long long units, int ctas, long long unit) {
-  int c = (int)(unit * ctas / units);
-  while (c + 1 < ctas && run_begin(units, ctas, c + 1) <= unit) ++c;
-  while (c > 0 && run_begin(units, ctas, c) > unit) --c;
-  return c;
-}
-
 // A row's sum l goes by the scores alone and its reference m by score and page exponent: with pages whose exponents lie 230 apart 2^d, d <= 0, may
 // be nothing where l 2^d is not.  In two halves.
 __device__ __forceinline__ float times_power(float l, float d) {
@@ -136,25 +158,26 @@ __device__ __forceinline__ float times_power(float l, float d) {
 }
 constexpr float kFar = 40.f;      // a page whose largest x lies as far below m adds nothing to a row's O; to its l perhaps
 
-// where packed row r (of a sequence whose rows begin at `first`) of KV head h is stored
-__device__ __forceinline__ void store_row_piece(const CacheAttnArgs& a, int first, int r, int head, int d, float4 v) {
-  const int t = r / a.G, g = r - t * a.G;
-  const long long at = (long long)(first + t) * a.out_row + (long long)(head * a.G + g) * a.out_head + d;
+// place in [n_rows][Hq] of packed row r (of a sequence whose rows begin at `first`) of KV head h: row and head
+struct RowHead { int row, head; };
+__device__ __forceinline__ RowHead row_head(const CacheAttnArgs& a, int first, int r, int h) {
+  const int t = by_group(a, r);
+  return {first + t, h * a.G + (r - t * a.G)};
+}
+__device__ __forceinline__ void store_row_piece(const CacheAttnArgs& a, RowHead p, int d, float4 v) {
+  const long long at = (long long)p.row * a.out_row + (long long)p.head * a.out_head + d;
   if (a.out_fp32) *reinterpret_cast<float4*>(static_cast<float*>(a.out) + at) = v;
   else {
     const __nv_bfloat162 x = __floats2bfloat162_rn(v.x, v.y), y = __floats2bfloat162_rn(v.z, v.w);
     *reinterpret_cast<uint2*>(static_cast<bf16*>(a.out) + at) = make_uint2(*reinterpret_cast<const uint32_t*>(&x), *reinterpret_cast<const uint32_t*>(&y));
   }
 }
-__device__ __forceinline__ void store_lse(const CacheAttnArgs& a, int first, int r, int head, float m, float l) {
-  if (a.lse == nullptr) return;
-  const int t = r / a.G, g = r - t * a.G;
-  a.lse[(long long)(first + t) * a.Hq + head * a.G + g] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+__device__ __forceinline__ void store_lse(const CacheAttnArgs& a, RowHead p, float m, float l) {
+  if (a.lse != nullptr) a.lse[(long long)p.row * a.Hq + p.head] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
 }
 #endif
 
-int launch_cache_attention_few(const CacheAttnArgs& a, int cols, int ctas, cudaStream_t st);
-int launch_cache_attention_many(const CacheAttnArgs& a, int ctas, cudaStream_t st);
-int launch_cache_attention_join(const CacheAttnArgs& a, int width, int ctas, cudaStream_t st);
+int launch_cache_attention_few(const CacheAttnArgs& a, int cols, cudaStream_t st);
+int launch_cache_attention_many(const CacheAttnArgs& a, bool behind_few, cudaStream_t st);
 
 }  // namespace vs
