@@ -89,26 +89,6 @@ __device__ __forceinline__ float max3_nan(float a, float b, float c) {
   asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
 }
-// 2^y of a pair, y <= 16: by the special-function unit (four lanes a clock and scheduler, what bounds the softmax), and by arithmetic for a share of the
-// weights: y = n + f, n the nearest integer, 2^f by the polynomial of degree 4 with the least relative error on [-1/2, 1/2] (Remez exchange;
-// 2.6e-6, against half a step of 2^-12 that rounding to fp16 adds), n added to the exponent.  Below 2^-126: 2^-126.
-constexpr int kByUnit = 8;             // of eight pairs
-__device__ __forceinline__ float2 power_by_unit(uint64_t y) {
-  const float2 v = f32x2_parts(y);
-  return make_float2(ex2_approx(v.x), ex2_approx(v.y));
-}
-__device__ __forceinline__ float2 power_by_polynomial(uint64_t y) {
-  const float2 v = f32x2_parts(y);
-  const uint64_t t = f32x2(fmaxf(v.x, -126.f), fmaxf(v.y, -126.f));
-  const uint64_t n = add_f32x2(t, f32x2(12582912.f, 12582912.f));         // 1.5 * 2^23: the integer in the low bits
-  const uint64_t f = fma_f32x2(add_f32x2(n, f32x2(-12582912.f, -12582912.f)), f32x2(-1.f, -1.f), t);
-  uint64_t q = fma_f32x2(f, f32x2(0.009570102207f, 0.009570102207f), f32x2(0.055917859077f, 0.055917859077f));
-  q = fma_f32x2(q, f, f32x2(0.240247443318f, 0.240247443318f));
-  q = fma_f32x2(q, f, f32x2(0.693121790886f, 0.693121790886f));
-  q = fma_f32x2(q, f, f32x2(0.999999284744f, 0.999999284744f));
-  const float2 p = f32x2_parts(q), e = f32x2_parts(n);
-  return make_float2(__int_as_float(__float_as_int(p.x) + (__float_as_int(e.x) << 23)), __int_as_float(__float_as_int(p.y) + (__float_as_int(e.y) << 23)));
-}
 __device__ __forceinline__ uint32_t half2_of(float lo, float hi) {
   const __half2 h = __floats2half2_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&h);
@@ -486,10 +466,10 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attention_tc_kernel(const _
 #pragma unroll
           for (int c = 0; c < kPage / 4; ++c) {
             const int k = 2 * (q * (kPage / 4) + c);
-            const uint64_t y = fma_f32x2(f32x2(__uint_as_float(x[k]), __uint_as_float(x[k + 1])), f2, c2);
-            const float2 w = (c & 7) >= kByUnit ? power_by_polynomial(y) : power_by_unit(y);
-            sum[c & 1] = add_f32x2(sum[c & 1], f32x2(w.x, w.y));
-            pw[c] = half2_of(w.x, w.y);
+            const float2 y = f32x2_parts(fma_f32x2(f32x2(__uint_as_float(x[k]), __uint_as_float(x[k + 1])), f2, c2));
+            const float w0 = ex2_approx(y.x), w1 = ex2_approx(y.y);
+            sum[c & 1] = add_f32x2(sum[c & 1], f32x2(w0, w1));
+            pw[c] = half2_of(w0, w1);
           }
           if (rare) {
 #pragma unroll

@@ -37,7 +37,8 @@ __device__ __forceinline__ void values(const Raw<float>& r, float (&x)[8]) { loa
 
 template <typename T, int kRows>
 __global__ void __launch_bounds__(kThreads) rope_axes_kernel(const __grid_constant__ RopeAxesArgs a) {
-  __shared__ float2 turn[kRows][kMaxHalf];
+  // (eight pairs and 16 bytes of nothing: what eight lanes read side by side lies in different banks)
+  __shared__ __align__(16) float2 turn[kRows][kMaxHalf / 8 * 10];
   const int row0 = (int)blockIdx.x * kRows, n_rows = min(kRows, a.rows - row0);
   const int per_head = a.half / 8, per_row = a.heads * per_head, n = n_rows * per_row;      // pieces of eight pairs
   const T* x = static_cast<const T*>(a.x);
@@ -65,7 +66,7 @@ __global__ void __launch_bounds__(kThreads) rope_axes_kernel(const __grid_consta
     const double t = (double)a.positions[(long long)a.axis[k] * a.pos_stride + row0 + row] * a.turns[k];
     float s, c;
     sincospif(2.f * (float)(t - rint(t)), &s, &c);
-    turn[row][k] = make_float2(c, a.inverse ? -s : s);
+    turn[row][k + (k >> 3) * 2] = make_float2(c, a.inverse ? -s : s);
   }
   __syncthreads();
   for (int i0 = 0; i0 < n; i0 += kRows * kThreads) {
@@ -78,11 +79,14 @@ __global__ void __launch_bounds__(kThreads) rope_axes_kernel(const __grid_consta
       float l[8], h[8], y[8], z[8];
       values(lo[u], l);
       values(hi[u], h);
+      const float4* cs = reinterpret_cast<const float4*>(&turn[p.row][p.k + (p.k >> 3) * 2]);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float2 cs = turn[p.row][p.k + e];
-        y[e] = l[e] * cs.x - h[e] * cs.y;
-        z[e] = h[e] * cs.x + l[e] * cs.y;
+      for (int e = 0; e < 8; e += 2) {
+        const float4 t = cs[e / 2];
+        y[e] = l[e] * t.x - h[e] * t.y;
+        z[e] = h[e] * t.x + l[e] * t.y;
+        y[e + 1] = l[e + 1] * t.z - h[e + 1] * t.w;
+        z[e + 1] = h[e + 1] * t.z + l[e + 1] * t.w;
       }
       T* at = out + (long long)(row0 + p.row) * a.out_row + (long long)p.head * a.out_head + p.k;
       store8(at, y);

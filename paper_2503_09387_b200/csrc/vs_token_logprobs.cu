@@ -61,6 +61,9 @@ struct Part {
   }
 };
 
+__device__ __forceinline__ float of_ordered(uint32_t o) {               // (NaN of 0)
+  return o == 0u ? __int_as_float(0x7fc00000) : __uint_as_float((o & 0x80000000u) ? o & 0x7fffffffu : ~o);
+}
 __device__ __forceinline__ uint32_t ordered(float v) {                 // ascending with v; NaN below every number, -0 = 0
   if (v != v) return 0u;
   const uint32_t b = __float_as_uint(v + 0.f);
@@ -137,6 +140,7 @@ __global__ void __launch_bounds__(kThreads, 2) token_logprobs_kernel(const __gri
   float best_x = -INFINITY, ref = 0.f, sum = 0.f, sum_u = 0.f;         // ref: the thread's reference
   int n_before = 0;
   bool odd = false;
+  float zero = 0.f;
   for (int v = v0 + tid; v < v1; v += U * kThreads) {
     uint4 now[U];
 #pragma unroll
@@ -155,7 +159,12 @@ __global__ void __launch_bounds__(kThreads, 2) token_logprobs_kernel(const __gri
       best_x = fmaxf(best_x, x);
       n_before += x > xt ? 1 : 0;
       ties = ties || x == xt;
-      odd = odd || !(x <= 3.402823466e38f);                            // NaN or +inf
+      zero = fmaf(x, 0.f, zero);                                        // (NaN by a NaN or an infinity)
+    }
+    if (!(zero == 0.f)) {                                              // rarely, but for masked rows: NaN or +inf?
+      zero = 0.f;
+#pragma unroll
+      for (int i = 0; i < E; ++i) odd = odd || !(element<T>(now[i / V], i % V) <= 3.402823466e38f);
     }
     if (ties) {                                                        // equal ones of a lower index
 #pragma unroll
@@ -346,14 +355,9 @@ __global__ void __launch_bounds__(kThreads, 2) token_logprobs_kernel(const __gri
     if (a.entropy != nullptr) a.entropy[row_i] = bad ? nan : (empty ? 0.f : fmaxf(log_sum - whole.u / (1.f + whole.s), 0.f));
   }
   if (tid < k) {
-    const int i = 0x7fffffff - (int)(uint32_t)best[tid];
-    if (a.top_index != nullptr) a.top_index[(long long)row_i * k + tid] = i;
-    if (a.top_logprob != nullptr) {
-      float x;
-      if constexpr (sizeof(T) == 4) x = row[i];
-      else x = __bfloat162float(row[i]);
-      a.top_logprob[(long long)row_i * k + tid] = logprob_of(x);
-    }
+    const unsigned long long key = best[tid];
+    if (a.top_index != nullptr) a.top_index[(long long)row_i * k + tid] = 0x7fffffff - (int)(uint32_t)key;
+    if (a.top_logprob != nullptr) a.top_logprob[(long long)row_i * k + tid] = logprob_of(of_ordered((uint32_t)(key >> 32)));
   }
 }
 
@@ -390,9 +394,14 @@ extern "C" int vs_token_logprobs(const vs_scores* x, void* cuda_stream) {
   OnDevice on(x->device);
   if (!on.ok) return VS_ERR_CUDA;
   ScoreArgs a = {x->logits, x->tokens, x->logprob, x->entropy, x->top_logprob, x->rank, x->top_index, x->row_stride, x->rows, x->vocab, x->top, 1};
-  // CTAs of a row: as many as leave none of the first 296 places (two an SM) waiting, no more than give a thread something to read
-  const int vectors = (int)((x->vocab + 16 / el - 1) / (16 / el));
-  while (a.cluster < kMaxCluster && 2ll * a.cluster * x->rows <= 296 && vectors > 2 * a.cluster * kThreads) a.cluster *= 2;
+  // CTAs of a row, measured for rows of 5000 to 152064 logits (fp32, top 0 to 20).  A part of at least 4096 vectors keeps a CTA busy for longer than joining
+  // the parts takes (one row of 32000: 9.2 us in one part, 8.9 in four; 64 rows 10.2, 11.3).  Eight parts up to eight rows (one row of 152064: 26.6 us in one,
+  // 13.7 in four, 13.3 in eight; sixteen rows 28.2, 14.5, 17.1: clusters of eight wait for one another's places), four up to 74 (40 rows
+  // 29.3, 20.5), then as many CTAs as there are SMs are at work anyway: two where the last round over the SMs would be less than half full
+  // (197 rows 42.3, 39.8; 148 rows 27.9, 28.4; 256 rows 42.9, 50.6).
+  const int vectors = (int)((x->vocab + 16 / el - 1) / (16 / el)), last = x->rows % 148;
+  const int most = x->rows <= 8 ? 8 : (x->rows <= 74 ? 4 : (x->rows > 148 && last != 0 && last <= 74 ? 2 : 1));
+  while (a.cluster < most && vectors >= 8192 * a.cluster) a.cluster *= 2;
   const bool vector = aligned(x->logits, 16) && (x->row_stride * (int64_t)el) % 16 == 0;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   if (x->dtype == 1) return vector ? launch<float, true>(a, st) : launch<float, false>(a, st);
