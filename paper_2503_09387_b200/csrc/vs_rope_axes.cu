@@ -3,26 +3,27 @@
 // Pair k of a head, (x_k, x_{k + D/2}), turns by the angle  pos[axis(k)] theta^(-2k / D): the frequency goes by the pair, the
 // position by the axis that the pair belongs to.  The inverse turns back, which is also the gradient with respect to x.
 //
-// What bounds it: the rows' bytes once in and once out; a call of one row is a launch and two dependent loads.  A block takes
-// kRows rows: its threads ask for their pieces of the rows first (16 bytes of either half), work out an angle each while those are on
-// their way, and turn every head of the rows by the angles in shared memory.  Frequencies and axes of the pairs come with the
-// launch.  A far position loses nothing: the angle is formed in turns in fp64, and only the fraction of a turn goes on in fp32.
+// What bounds it: the rows' bytes once in and once out; a call of one row is a launch and two dependent loads.  A warp takes some heads of a
+// row and asks for its pieces of them first (16 bytes of either half), works out the angles while those are on their way -- a lane some pairs'
+// each, once for all of the warp's heads -- and hands them round through shared memory: a lane turns the same eight pairs of every head
+// that it meets, so it keeps them in registers.  No warp waits for another.  A far position loses nothing: the angle is
+// formed in turns in fp64, and only the fraction of a turn goes on in fp32.
 #include "vs_operators.cuh"
 
 namespace vs {
 
 namespace {
 
-constexpr int kThreads = 256, kMaxHalf = 128;
+constexpr int kWarps = 4, kMaxHalf = 128, kLoads = 4;
 
 struct RopeAxesArgs {
   const void* x;
   void* out;
   const int64_t* positions;
   long long x_row, x_head, out_row, out_head, pos_stride;
-  int rows, heads, half, inverse;
-  unsigned char axis[kMaxHalf];       // of a pair
-  double turns[kMaxHalf];             // theta^(-2k / D) / 2 pi
+  int rows, heads, half, inverse, per_row, beside;     // warps of a row; heads that a warp takes side by side
+  uint32_t axis[kMaxHalf / 16];        // of a pair, two bits each
+  double turns[32], step;              // theta^(-2k / D) / 2 pi of the first 32 pairs, and theta^(-64 / D)
 };
 
 // eight elements as they are stored
@@ -35,86 +36,82 @@ template <> struct Raw<float> {
 __device__ __forceinline__ void values(const Raw<bf16>& r, float (&x)[8]) { load8(reinterpret_cast<const bf16*>(&r), x); }
 __device__ __forceinline__ void values(const Raw<float>& r, float (&x)[8]) { load8(reinterpret_cast<const float*>(&r), x); }
 
-template <typename T, int kRows>
-__global__ void __launch_bounds__(kThreads) rope_axes_kernel(const __grid_constant__ RopeAxesArgs a) {
+template <typename T>
+__global__ void __launch_bounds__(32 * kWarps) rope_axes_kernel(const __grid_constant__ RopeAxesArgs a) {
   // (eight pairs and 16 bytes of nothing: what eight lanes read side by side lies in different banks)
-  __shared__ __align__(16) float2 turn[kRows][kMaxHalf / 8 * 10];
-  const int row0 = (int)blockIdx.x * kRows, n_rows = min(kRows, a.rows - row0);
-  const int per_head = a.half / 8, per_row = a.heads * per_head, n = n_rows * per_row;      // pieces of eight pairs
-  const T* x = static_cast<const T*>(a.x);
-  T* out = static_cast<T*>(a.out);
-  struct Piece { int row, head, k; };
-  auto piece = [&](int i) {
-    Piece p;
-    p.row = i / per_row;
-    const int j = i - p.row * per_row;
-    p.head = j / per_head;
-    p.k = (j - p.head * per_head) * 8;
-    return p;
-  };
-  Raw<T> lo[kRows], hi[kRows];
-  auto load = [&](int i, Raw<T>& l, Raw<T>& h) {
-    const Piece p = piece(i);
-    const T* at = x + (long long)(row0 + p.row) * a.x_row + (long long)p.head * a.x_head + p.k;
-    l.load(at);
-    h.load(at + a.half);
-  };
+  __shared__ __align__(16) float2 turn[kWarps][kMaxHalf / 8 * 10];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const long long w = (long long)blockIdx.x * kWarps + warp;
+  const int row = (int)(w / a.per_row), part = (int)(w - (long long)row * a.per_row);
+  if (row >= a.rows) return;
+  const int per_head = a.half / 8, mine = lane / per_head, k0 = (lane - mine * per_head) * 8;      // the lane's head of those side by side
+  const int head0 = part * kLoads * a.beside + mine;
+  const bool idle = mine >= a.beside;
+  const T* x = static_cast<const T*>(a.x) + (long long)row * a.x_row + k0;
+  T* out = static_cast<T*>(a.out) + (long long)row * a.out_row + k0;
+  Raw<T> lo[kLoads], hi[kLoads];
 #pragma unroll
-  for (int u = 0; u < kRows; ++u) if ((int)threadIdx.x + u * kThreads < n) load((int)threadIdx.x + u * kThreads, lo[u], hi[u]);
-  for (int i = threadIdx.x; i < n_rows * a.half; i += kThreads) {
-    const int row = i / a.half, k = i - row * a.half;
-    const double t = (double)a.positions[(long long)a.axis[k] * a.pos_stride + row0 + row] * a.turns[k];
+  for (int u = 0; u < kLoads; ++u) {
+    const int head = head0 + u * a.beside;
+    if (idle || head >= a.heads) continue;
+    lo[u].load(x + (long long)head * a.x_head);
+    hi[u].load(x + (long long)head * a.x_head + a.half);
+  }
+  double turns = a.turns[lane];
+  for (int k = lane; k < a.half; k += 32, turns *= a.step) {
+    const int axis = (int)(a.axis[k >> 4] >> (2 * (k & 15))) & 3;
+    const double t = (double)a.positions[(long long)axis * a.pos_stride + row] * turns;
     float s, c;
     sincospif(2.f * (float)(t - rint(t)), &s, &c);
-    turn[row][k + (k >> 3) * 2] = make_float2(c, a.inverse ? -s : s);
+    turn[warp][k + (k >> 3) * 2] = make_float2(c, a.inverse ? -s : s);
   }
-  __syncthreads();
-  for (int i0 = 0; i0 < n; i0 += kRows * kThreads) {
+  __syncwarp();
+  if (idle) return;
+  float4 cs[4];
 #pragma unroll
-    for (int u = 0; u < kRows; ++u) {
-      const int i = i0 + (int)threadIdx.x + u * kThreads;
-      if (i >= n) continue;
-      if (i0 > 0) load(i, lo[u], hi[u]);
-      const Piece p = piece(i);
-      float l[8], h[8], y[8], z[8];
-      values(lo[u], l);
-      values(hi[u], h);
-      const float4* cs = reinterpret_cast<const float4*>(&turn[p.row][p.k + (p.k >> 3) * 2]);
+  for (int e = 0; e < 4; ++e) cs[e] = reinterpret_cast<const float4*>(&turn[warp][k0 + (k0 >> 3) * 2])[e];
 #pragma unroll
-      for (int e = 0; e < 8; e += 2) {
-        const float4 t = cs[e / 2];
-        y[e] = l[e] * t.x - h[e] * t.y;
-        z[e] = h[e] * t.x + l[e] * t.y;
-        y[e + 1] = l[e + 1] * t.z - h[e + 1] * t.w;
-        z[e + 1] = h[e + 1] * t.z + l[e + 1] * t.w;
-      }
-      T* at = out + (long long)(row0 + p.row) * a.out_row + (long long)p.head * a.out_head + p.k;
-      store8(at, y);
-      store8(at + a.half, z);
+  for (int u = 0; u < kLoads; ++u) {
+    const int head = head0 + u * a.beside;
+    if (head >= a.heads) break;
+    float l[8], h[8], y[8], z[8];
+    values(lo[u], l);
+    values(hi[u], h);
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) {
+      const float4 t = cs[e / 2];
+      y[e] = l[e] * t.x - h[e] * t.y;
+      z[e] = h[e] * t.x + l[e] * t.y;
+      y[e + 1] = l[e + 1] * t.z - h[e + 1] * t.w;
+      z[e + 1] = h[e + 1] * t.z + l[e + 1] * t.w;
     }
+    T* at = out + (long long)head * a.out_head;
+    store8(at, y);
+    store8(at + a.half, z);
   }
 }
 
 // The axis whose position turns pair k: the sections one behind the other, or the pairs dealt to the axes in turn, one that has its share
 // left out.
-void deal_axes(const int32_t* sections, int n_axes, int half, bool interleaved, unsigned char* axis) {
+void deal_axes(const int32_t* sections, int n_axes, int half, bool interleaved, uint32_t* axis) {
   int left[VS_MAX_AXES];
   for (int i = 0; i < n_axes; ++i) left[i] = sections[i];
   for (int k = 0, i = 0; k < half; i = interleaved ? i + 1 : i) {
     if (i == n_axes) i = 0;
     if (left[i] == 0) { if (!interleaved) ++i; continue; }
     --left[i];
-    axis[k++] = (unsigned char)i;
+    axis[k >> 4] |= (uint32_t)i << (2 * (k & 15));
+    ++k;
   }
 }
 
-// theta^(-2k / D) / 2 pi of every pair: kept by the calling thread for its next call of the same base and size (64 powers take longer
+// theta^(-2k / D) / 2 pi of the first pairs: kept by the calling thread for its next call of the same base and size (32 powers take longer
 // than the launch)
-struct Turns { double theta = 0.0; int half = 0; double of[kMaxHalf]; };
+struct Turns { double theta = 0.0; int half = 0; double of[32]; };
 const double* turns_of(double theta, int half) {
   static thread_local Turns kept;
   if (kept.theta != theta || kept.half != half) {
-    for (int k = 0; k < half; ++k) kept.of[k] = std::pow(theta, -(double)k / half) * 0.15915494309189533577;
+    for (int k = 0; k < 32; ++k) kept.of[k] = std::pow(theta, -(double)k / half) * 0.15915494309189533577;
     kept.theta = theta;
     kept.half = half;
   }
@@ -146,16 +143,20 @@ extern "C" int vs_rope_axes(const vs_rope* r, void* cuda_stream) {
   if (!aligned(r->x, 16) || !aligned(r->out, 16)) return VS_ERR_INVALID_ARG;
   OnDevice on(r->device);
   if (!on.ok) return VS_ERR_CUDA;
-  RopeAxesArgs a;
+  RopeAxesArgs a = {};
   a.x = r->x; a.out = r->out; a.positions = r->positions;
   a.x_row = strides[0]; a.x_head = strides[1]; a.out_row = strides[2]; a.out_head = strides[3]; a.pos_stride = r->pos_stride;
   a.rows = r->rows; a.heads = r->heads; a.half = half; a.inverse = r->inverse != 0;
+  a.beside = 32 / (half / 8);
+  a.per_row = (r->heads + kLoads * a.beside - 1) / (kLoads * a.beside);
   deal_axes(r->sections, r->n_axes, half, r->interleaved != 0, a.axis);
   const double* turns = turns_of(r->theta, half);
-  for (int k = 0; k < half; ++k) a.turns[k] = turns[k];
+  for (int k = 0; k < 32; ++k) a.turns[k] = turns[k];
+  a.step = std::pow(r->theta, -32.0 / half);
+  const long long blocks = ((long long)r->rows * a.per_row + kWarps - 1) / kWarps;
+  if (blocks > 0x7fffffffll) return VS_ERR_UNSUPPORTED;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  const int blocks = r->rows;
-  if (r->dtype == 1) rope_axes_kernel<float, 1><<<blocks, kThreads, 0, st>>>(a);
-  else rope_axes_kernel<bf16, 1><<<blocks, kThreads, 0, st>>>(a);
+  if (r->dtype == 1) rope_axes_kernel<float><<<(unsigned)blocks, 32 * kWarps, 0, st>>>(a);
+  else rope_axes_kernel<bf16><<<(unsigned)blocks, 32 * kWarps, 0, st>>>(a);
   return launched();
 }

@@ -24,7 +24,8 @@ namespace {
 constexpr int kThreads = 512, kWarps = kThreads / 32, kTop = VS_MAX_TOP, kMaxCluster = 8;
 constexpr int kAbove = 1024, kEqual = 256;             // candidates above the bound, and equal to it, that are kept
 constexpr uint32_t kLeastNumber = 0x00800000u;         // the most negative finite logit, as ordered() has it; -inf is one less, NaN 0
-constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f, kHuge = 1e38f;
+constexpr int kBins = 64;
 
 struct ScoreArgs {
   const void* logits;
@@ -75,11 +76,33 @@ __device__ __forceinline__ unsigned long long key_of(uint32_t o, int i) { return
 template <typename T>
 struct Vec { static constexpr int n = 16 / (int)sizeof(T); };
 
-// the logits of vector i of a row: those behind its end as -inf
+// the logits of vector i of a row, all of which are there
+template <typename T, bool kVector>
+__device__ __forceinline__ uint4 fetch_whole(const T* row, int i) {
+  constexpr int V = Vec<T>::n;
+  if constexpr (kVector) {
+    return __ldg(reinterpret_cast<const uint4*>(row) + i);
+  } else {
+    uint32_t w[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if constexpr (sizeof(T) == 4) {
+        w[j] = __float_as_uint(row[i * V + j]);
+      } else {
+        const uint16_t* r = reinterpret_cast<const uint16_t*>(row) + i * V + 2 * j;
+        w[j] = (uint32_t)r[0] | ((uint32_t)r[1] << 16);
+      }
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  }
+}
+// those of any vector: -inf behind the end of the row
 template <typename T, bool kVector>
 __device__ __forceinline__ uint4 fetch(const T* row, int i, int vocab) {
   constexpr int V = Vec<T>::n;
   if (kVector && (i + 1) * V <= vocab) return __ldg(reinterpret_cast<const uint4*>(row) + i);
+  const uint32_t nothing = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;
+  if (i * V >= vocab) return make_uint4(nothing, nothing, nothing, nothing);
   uint32_t w[4];
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
@@ -109,10 +132,22 @@ struct Shared {
   unsigned long long above[kAbove], equal[kEqual + kTop], best[kMaxCluster * kTop];
   Part part[kWarps];
   int before[kWarps], odd[kWarps];     // logits that come before the token; whether a NaN or +inf was met
+  uint32_t most[kWarps], least[kWarps];                                 // of the threads' maxima
+  int bins[3][kBins];
+  short holder[kThreads];              // threads whose maximum reaches the bound
   Part whole;                          // this CTA's part of the row, for the cluster's first
-  int n_before, n_odd, n_above, n_equal;
+  int n_before, n_odd, n_above, n_equal, n_holders;
   uint32_t bound;
 };
+
+// the next larger number (NaN of +inf)
+__device__ __forceinline__ float next_up(float x) { return x == INFINITY ? __int_as_float(0x7fc00000) : of_ordered(ordered(x) + 1u); }
+// the larger one, NaN if either is
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float m;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(a), "f"(b));
+  return m;
+}
 
 template <typename T, bool kVector>
 __global__ void __launch_bounds__(kThreads, 2) token_logprobs_kernel(const __grid_constant__ ScoreArgs a) {
@@ -123,89 +158,110 @@ __global__ void __launch_bounds__(kThreads, 2) token_logprobs_kernel(const __gri
   const T* row = static_cast<const T*>(a.logits) + (long long)row_i * a.row_stride;
   const int nv = (a.vocab + V - 1) / V;
   const int v0 = (int)((long long)nv * rank / C), v1 = (int)((long long)nv * (rank + 1) / C);
+  const int whole_v = min(v1, a.vocab / V), steps = (v1 - v0 + U * kThreads - 1) / (U * kThreads);
+  // the vectors of one step: without a question where all threads have all of theirs
+  uint4 next[U];
+  auto load = [&](int v) {
+    if (v - tid + U * kThreads <= whole_v) {
+#pragma unroll
+      for (int j = 0; j < U; ++j) next[j] = fetch_whole<T, kVector>(row, v + j * kThreads);
+    } else {
+#pragma unroll
+      for (int j = 0; j < U; ++j) next[j] = fetch<T, kVector>(row, v + j * kThreads, v + j * kThreads < v1 ? a.vocab : 0);
+    }
+  };
+  load(v0 + tid);
   const int token = a.tokens != nullptr ? a.tokens[row_i] : -1;
   const bool has_token = token >= 0 && token < a.vocab;
-  const uint4 nothing = sizeof(T) == 4 ? make_uint4(0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u) : make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u);
-  uint4 next[U];
-#pragma unroll
-  for (int j = 0; j < U; ++j) next[j] = v0 + tid + j * kThreads < v1 ? fetch<T, kVector>(row, v0 + tid + j * kThreads, a.vocab) : nothing;
-  float xt = INFINITY;                 // (no token: nothing comes before it)
+  const float nan = __int_as_float(0x7fc00000);
+  float xt = nan;                      // (no token: nothing comes before it)
   if (has_token) {
     if constexpr (sizeof(T) == 4) xt = row[token];
     else xt = __bfloat162float(row[token]);
   }
-  const bool xt_nan = xt != xt;
+  const bool xt_nan = has_token && xt != xt;
+  // what reaches this comes before the token: its logit in the vectors ahead of the token's, the next larger one from there on
+  const float behind = next_up(xt);
+  const int token_v = has_token ? token / V : 0, ahead = min(token_v, v1);
 
   // ---- one pass: largest, sums of the others, place of the token -----------------------------------------------
-  float best_x = -INFINITY, ref = 0.f, sum = 0.f, sum_u = 0.f;         // ref: the thread's reference
+  float best_x = -INFINITY, ref = 0.f, ref2 = 0.f, off = 0.f, sum = 0.f, sum_u = 0.f;  // ref2 = ref log2e - off, as it is rounded
   int n_before = 0;
-  bool odd = false;
-  float zero = 0.f;
-  for (int v = v0 + tid; v < v1; v += U * kThreads) {
-    uint4 now[U];
-#pragma unroll
-    for (int j = 0; j < U; ++j) {
-      now[j] = next[j];
-      const int w = v + (U + j) * kThreads;
-      next[j] = w < v1 ? fetch<T, kVector>(row, w, a.vocab) : nothing;
-    }
+  auto shift_sums = [&](float by) {    // by so many powers of two
+    by = fmaxf(by, -1000.f);
+    const float r = ex2_approx(by);
+    sum_u = r * fmaf(by, sum, sum_u);
+    sum *= r;
+  };
+  for (int step = 0, v = v0 + tid; step < steps; ++step, v += U * kThreads) {
     const float was = best_x;
-    bool ties = false;
     float y[E];                                                         // what is summed: the logit, or the largest so far that it replaces
 #pragma unroll
-    for (int i = 0; i < E; ++i) {
-      const float x = element<T>(now[i / V], i % V);
-      y[i] = fminf(best_x, x);
-      best_x = fmaxf(best_x, x);
-      n_before += x > xt ? 1 : 0;
-      ties = ties || x == xt;
-      zero = fmaf(x, 0.f, zero);                                        // (NaN by a NaN or an infinity)
-    }
-    if (!(zero == 0.f)) {                                              // rarely, but for masked rows: NaN or +inf?
-      zero = 0.f;
+    for (int j = 0; j < U; ++j) {
+      const float reach = v + j * kThreads < ahead ? xt : behind;
 #pragma unroll
-      for (int i = 0; i < E; ++i) odd = odd || !(element<T>(now[i / V], i % V) <= 3.402823466e38f);
-    }
-    if (ties) {                                                        // equal ones of a lower index
-#pragma unroll
-      for (int i = 0; i < E; ++i) n_before += element<T>(now[i / V], i % V) == xt && (v + (i / V) * kThreads) * V + i % V < token ? 1 : 0;
-    }
-    if (xt_nan) {                                                      // behind every number, and NaN of a lower index
-#pragma unroll
-      for (int i = 0; i < E; ++i) {
-        const int w = v + (i / V) * kThreads, at = w * V + i % V;
-        const float x = element<T>(now[i / V], i % V);
-        n_before += w < v1 && at < a.vocab && (x == x || at < token) ? 1 : 0;
+      for (int e = 0; e < V; ++e) {
+        const float x = element<T>(next[j], e);
+        y[j * V + e] = fminf(best_x, x);
+        best_x = max_nan(best_x, x);
+        n_before += x >= reach ? 1 : 0;
       }
     }
+    if (step + 1 < steps) load(v + U * kThreads);
     if (best_x > -INFINITY && (was == -INFINITY || best_x - ref > 40.f)) {
-      const float d = fmaxf(ref - best_x, -1000.f), r = was == -INFINITY ? 0.f : exp2f(d * kLog2e);
-      sum_u = r > 0.f ? r * (sum_u + d * sum) : 0.f;
-      sum *= r;
-      ref = best_x;
+      const bool finite = fabsf(best_x) < kHuge;
+      const float to2 = finite ? best_x * kLog2e : 0.f, to_off = finite ? fmaf(best_x, kLog2e, -to2) : 0.f;
+      if (was != -INFINITY) shift_sums(fmaf(ref - best_x, kLog2e, to_off - off));
+      ref = best_x; ref2 = to2; off = to_off;
     }
     float s = 0.f, u = 0.f;
+    if (fabsf(ref) < kHuge) {
 #pragma unroll
-    for (int i = 0; i < E; ++i) {
-      const float d = fmaxf(y[i] - ref, -1000.f), e = ex2_approx(d * kLog2e);           // (-inf: 0, and 0 in u)
-      s += e;
-      u = fmaf(d, e, u);
+      for (int i = 0; i < E; ++i) {
+        const float d = fmaxf(fmaf(y[i], kLog2e, -ref2), -1000.f), e = ex2_approx(d);    // (-inf: 0, and 0 in u)
+        s += e;
+        u = fmaf(d, e, u);
+      }
+    } else {                                                           // a row of the type's lowest value: it times log2e would be infinite
+#pragma unroll
+      for (int i = 0; i < E; ++i) {
+        const float d = fmaxf(y[i] - ref, -1000.f) * kLog2e, e = ex2_approx(d);
+        s += e;
+        u = fmaf(d, e, u);
+      }
     }
     sum += s;
     sum_u += u;
   }
+  const bool odd = !(best_x < INFINITY);
+  if (best_x != best_x) {                                              // NaN among them: the largest number, for the alternatives
+    best_x = -INFINITY;
+    for (int v = v0 + tid; v < v1; v += kThreads) {
+      const uint4 w = fetch<T, kVector>(row, v, a.vocab);
+#pragma unroll
+      for (int e = 0; e < V; ++e) best_x = fmaxf(best_x, element<T>(w, e));
+    }
+  }
+  if (xt_nan) {                                                        // behind every number, and NaN of a lower index
+    for (int v = v0 + tid; v < v1; v += kThreads)
+      for (int i = v * V; i < min((v + 1) * V, a.vocab); ++i) n_before += (float)row[i] == (float)row[i] || i < token ? 1 : 0;
+  }
   Part p = {best_x, 0.f, 0.f, 0u};
   if (best_x > -INFINITY) {
-    const float d = ref - best_x, r = exp2f(d * kLog2e);               // (e^{-40} at least)
-    p.s = sum * r;
-    p.u = r * (sum_u + d * sum);
+    shift_sums(fmaf(ref - best_x, kLog2e, -off));                      // (2^-58 at the least)
+    p.s = sum;
+    p.u = sum_u * kLn2;
   }
   const uint32_t own_max = ordered(p.m);
+  if (has_token && token_v >= v0 && token_v < v1 && tid == 0)          // equal ones ahead of the token in its own vector
+    for (int i = token_v * V; i < token; ++i) n_before += (float)row[i] == xt ? 1 : 0;
   p.join_lanes(32);
   n_before = __reduce_add_sync(0xffffffffu, n_before);
-  odd = __any_sync(0xffffffffu, odd);
-  if (lane == 0) { sm.part[warp] = p; sm.before[warp] = n_before; sm.odd[warp] = odd; }
-  if (tid == 0) { sm.n_above = 0; sm.n_equal = 0; }
+  const bool any_odd = __any_sync(0xffffffffu, odd);
+  const uint32_t warp_max = __reduce_max_sync(0xffffffffu, own_max), warp_min = __reduce_min_sync(0xffffffffu, own_max);
+  if (lane == 0) { sm.part[warp] = p; sm.before[warp] = n_before; sm.odd[warp] = any_odd; sm.most[warp] = warp_max; sm.least[warp] = warp_min; }
+  if (tid < kBins) sm.bins[0][tid] = 0;
+  if (tid == 0) { sm.n_above = 0; sm.n_equal = 0; sm.n_holders = 0; }
   __syncthreads();
   if (warp == 0) {
     Part w = sm.part[lane & (kWarps - 1)];
@@ -218,35 +274,79 @@ __global__ void __launch_bounds__(kThreads, 2) token_logprobs_kernel(const __gri
   // ---- the best of this CTA's part -----------------------------------------------------------------------------
   const int k = a.top;
   if (k > 0) {
-    // a bound that at least k of the threads' maxima reach, bit by bit from the top (the last 14 bits would sharpen it little)
-    uint32_t bound = 0u;
-    for (int bit = 31; bit >= 14; --bit) {
-      const uint32_t higher = bound | (1u << bit);
-      if (__syncthreads_count(own_max >= higher) >= k) bound = higher;
-    }
-    bound = max(bound, kLeastNumber);
-    for (;;) {
-      // a warp reads a thread's logits again, its lanes side by side
-      for (unsigned left = __ballot_sync(0xffffffffu, own_max >= bound); left != 0u; left &= left - 1u) {
-        const int t = warp * 32 + __ffs(left) - 1;
-        for (int v = v0 + t + lane * kThreads; v < v1; v += 32 * kThreads) {
-          const uint4 w = fetch<T, kVector>(row, v, a.vocab);
+    // a bound that at least k of the threads' maxima reach, and few more: by counting them in 64 bins between the least and the largest, then
+    // again within the bin that holds the k-th, until that is near enough
+    uint32_t from = max(__reduce_min_sync(0xffffffffu, sm.least[lane & (kWarps - 1)]), kLeastNumber);
+    uint32_t to = max(__reduce_max_sync(0xffffffffu, sm.most[lane & (kWarps - 1)]), from);
+    uint32_t bound = from;
+    for (int round = 0, above = 0; ; ++round) {
+      const int shift = max(0, 26 - __clz(to - from));
+      if (tid < kBins) sm.bins[(round + 1) % 3][tid] = 0;
+      int* bins = sm.bins[round % 3];
+      if (own_max >= from && own_max <= to) atomicAdd(&bins[(own_max - from) >> shift], 1);
+      __syncthreads();
+      const int2 mine = reinterpret_cast<const int2*>(bins)[lane];
+      int reach = mine.x + mine.y;                                      // in this lane's bins and all above them
 #pragma unroll
-          for (int e = 0; e < V; ++e) {
-            const uint32_t o = ordered(element<T>(w, e));
-            const int i = v * V + e;
-            if (o < bound || i >= a.vocab) continue;
-            if (o > bound) { const int at = atomicAdd(&sm.n_above, 1); if (at < kAbove) sm.above[at] = key_of(o, i); }
-            else { const int at = atomicAdd(&sm.n_equal, 1); if (at < kEqual) sm.equal[at] = key_of(o, i); }
+      for (int o = 1; o < 32; o <<= 1) { const int t = __shfl_down_sync(0xffffffffu, reach, o); if (lane + o < 32) reach += t; }
+      const unsigned enough = __ballot_sync(0xffffffffu, above + reach >= k);
+      if (enough == 0u) { bound = kLeastNumber; break; }                // fewer than k threads have a number: all that there are
+      const int at = 31 - __clz(enough);
+      const int here = __shfl_sync(0xffffffffu, reach, at), upper = __shfl_sync(0xffffffffu, mine.y, at), both = __shfl_sync(0xffffffffu, mine.x + mine.y, at);
+      const bool in_upper = above + here - both + upper >= k;
+      const int bin = 2 * at + (in_upper ? 1 : 0), inside = in_upper ? upper : both - upper;
+      above += here - both + (in_upper ? 0 : upper);
+      from += (uint32_t)bin << shift;
+      to = min(to, from + ((1u << shift) - 1u));
+      bound = from;
+      if (shift == 0 || above + inside <= k + 12) break;
+    }
+    if (own_max >= bound) sm.holder[atomicAdd(&sm.n_holders, 1)] = (short)tid;
+    __syncthreads();
+    // the vectors of the threads that hold such a maximum, dealt to all threads (in little code: what runs once waits for its instructions)
+    const int per = (v1 - v0 + kThreads - 1) / kThreads, n_read = sm.n_holders * per;
+    for (;;) {
+      const float reach = of_ordered(bound);
+      auto look = [&](int v, const uint4& w) {
+        float most = element<T>(w, 0);
+#pragma unroll
+        for (int e = 1; e < V; ++e) most = fmaxf(most, element<T>(w, e));
+        if (!(most >= reach)) return;
+#pragma unroll 1
+        for (int at = v * V; at < min((v + 1) * V, a.vocab); ++at) {    // (few do)
+          const uint32_t o = ordered((float)row[at]);
+          if (o < bound) continue;
+          if (o > bound) { const int to = atomicAdd(&sm.n_above, 1); if (to < kAbove) sm.above[to] = key_of(o, at); }
+          else { const int to = atomicAdd(&sm.n_equal, 1); if (to < kEqual) sm.equal[to] = key_of(o, at); }
+        }
+      };
+      if (per > 32) {                                                   // many vectors a thread: four on their way at a time
+        for (int h = warp; h < sm.n_holders; h += kWarps) {
+          const int first = v0 + sm.holder[h];
+#pragma unroll 1
+          for (int v = first + lane * kThreads; v < v1; v += 128 * kThreads) {
+            uint4 w[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[j] = fetch<T, kVector>(row, v + 32 * j * kThreads, v + 32 * j * kThreads < v1 ? a.vocab : 0);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) look(v + 32 * j * kThreads, w[j]);
           }
+        }
+      } else {
+#pragma unroll 1
+        for (int i = tid; i < n_read; i += kThreads) {
+          const int h = i / per, v = v0 + sm.holder[h] + (i - h * per) * kThreads;
+          look(v, fetch<T, kVector>(row, v, v < v1 ? a.vocab : 0));
         }
       }
       __syncthreads();
       if (sm.n_above <= kAbove) break;
       // more than are kept: the k-th of those kept is a higher bound that k logits reach
+#pragma unroll 1
       for (int c = tid; c < kAbove; c += kThreads) {
         const unsigned long long mine = sm.above[c];
         int place = 0;
+#pragma unroll 1
         for (int i = 0; i < kAbove; ++i) place += sm.above[i] > mine ? 1 : 0;
         if (place == k - 1) sm.bound = (uint32_t)(mine >> 32);
       }
@@ -266,7 +366,7 @@ __global__ void __launch_bounds__(kThreads, 2) token_logprobs_kernel(const __gri
         for (int round = n_found > kEqual ? 0 : 1; round < 3; ++round) {
           const uint32_t wanted = round == 0 ? bound : (round == 1 ? kLeastNumber - 1u : 0u);
           for (int v = v0; v < v1 && have < k - n_above; v += 32) {
-            const uint4 w = v + lane < v1 ? fetch<T, kVector>(row, v + lane, a.vocab) : nothing;
+            const uint4 w = fetch<T, kVector>(row, v + lane, v + lane < v1 ? a.vocab : 0);
             uint32_t hits = 0u;
 #pragma unroll
             for (int e = 0; e < V; ++e)
@@ -289,11 +389,13 @@ __global__ void __launch_bounds__(kThreads, 2) token_logprobs_kernel(const __gri
     const int n = n_above + (n_above < k ? n_equal : 0);
     // in order, by counting; a part of few logits may hold fewer than k
     if (tid >= n && tid < k) sm.best[tid] = 0ull;
-    for (int c = tid; c < n; c += kThreads) {
+    for (int c = warp; c < n; c += kWarps) {
       const unsigned long long mine = c < n_above ? sm.above[c] : sm.equal[c - n_above];
       int place = 0;
-      for (int i = 0; i < n; ++i) place += (i < n_above ? sm.above[i] : sm.equal[i - n_above]) > mine ? 1 : 0;
-      if (place < k) sm.best[place] = mine;
+#pragma unroll 1
+      for (int i = lane; i < n; i += 32) place += (i < n_above ? sm.above[i] : sm.equal[i - n_above]) > mine ? 1 : 0;
+      place = __reduce_add_sync(0xffffffffu, place);
+      if (lane == 0 && place < k) sm.best[place] = mine;
     }
   }
   __syncthreads();
@@ -319,13 +421,21 @@ __global__ void __launch_bounds__(kThreads, 2) token_logprobs_kernel(const __gri
       const int c = tid / kTop, j = tid - c * kTop;
       if (c < C && j < k) {
         const unsigned long long mine = sm.best[c * kTop + j];
+        int lo[kMaxCluster], hi[kMaxCluster];
+#pragma unroll
+        for (int q = 0; q < kMaxCluster; ++q) { lo[q] = 0; hi[q] = q < C && q != c ? k : 0; }
+#pragma unroll 1
+        for (int step = 0; step < 6; ++step)                            // (of up to 32: side by side in all parts)
+#pragma unroll
+          for (int q = 0; q < kMaxCluster; ++q) {
+            const int mid = (lo[q] + hi[q]) >> 1;
+            const bool after = lo[q] < hi[q] && sm.best[q * kTop + min(mid, kTop - 1)] > mine;
+            lo[q] = after ? mid + 1 : lo[q];
+            hi[q] = after ? hi[q] : mid;
+          }
         int place = j;
-        for (int q = 0; q < C; ++q) {
-          if (q == c) continue;
-          int lo = 0, hi = k;
-          while (lo < hi) { const int mid = (lo + hi) >> 1; if (sm.best[q * kTop + mid] > mine) lo = mid + 1; else hi = mid; }
-          place += lo;
-        }
+#pragma unroll
+        for (int q = 0; q < kMaxCluster; ++q) place += lo[q];
         if (mine != 0ull && place < k) sm.above[place] = mine;
       }
       __syncthreads();
@@ -345,7 +455,6 @@ __global__ void __launch_bounds__(kThreads, 2) token_logprobs_kernel(const __gri
     all_before = __reduce_add_sync(0xffffffffu, lane < C ? sm.before[lane] : 0);
     bad = __any_sync(0xffffffffu, sm.odd[lane & (C - 1)] != 0);
   }
-  const float nan = __int_as_float(0x7fc00000);
   const float log_sum = log1pf(whole.s);                                // of e^{x - m}
   const bool empty = whole.m == -INFINITY;                              // nothing but -inf (and NaN)
   auto logprob_of = [&](float x) { return bad ? nan : (empty ? -INFINITY : (x - whole.m) - log_sum); };
@@ -394,13 +503,12 @@ extern "C" int vs_token_logprobs(const vs_scores* x, void* cuda_stream) {
   OnDevice on(x->device);
   if (!on.ok) return VS_ERR_CUDA;
   ScoreArgs a = {x->logits, x->tokens, x->logprob, x->entropy, x->top_logprob, x->rank, x->top_index, x->row_stride, x->rows, x->vocab, x->top, 1};
-  // CTAs of a row, measured for rows of 5000 to 152064 logits (fp32, top 0 to 20).  A part of at least 4096 vectors keeps a CTA busy for longer than joining
-  // the parts takes (one row of 32000: 9.2 us in one part, 8.9 in four; 64 rows 10.2, 11.3).  Eight parts up to eight rows (one row of 152064: 26.6 us in one,
-  // 13.7 in four, 13.3 in eight; sixteen rows 28.2, 14.5, 17.1: clusters of eight wait for one another's places), four up to 74 (40 rows
-  // 29.3, 20.5), then as many CTAs as there are SMs are at work anyway: two where the last round over the SMs would be less than half full
-  // (197 rows 42.3, 39.8; 148 rows 27.9, 28.4; 256 rows 42.9, 50.6).
-  const int vectors = (int)((x->vocab + 16 / el - 1) / (16 / el)), last = x->rows % 148;
-  const int most = x->rows <= 8 ? 8 : (x->rows <= 74 ? 4 : (x->rows > 148 && last != 0 && last <= 74 ? 2 : 1));
+  // CTAs of a row, measured for rows of 5000 to 152064 logits (fp32, five alternatives).  A part of at least 4096 vectors keeps a CTA busy for longer
+  // than joining the parts takes (one row of 32000: 7.9 us in one part, 9.0 in four; 64 rows of 5000 6.8, 11.3).  Eight parts up to eight rows (one
+  // row of 152064: 17.0 us in one, 11.3 in four, 10.6 in eight; sixteen rows 17.3, 11.6, 14.0: clusters of eight wait for one another's places), four
+  // while their CTAs are resident at once, two an SM (64 rows 21.7, 17.4; 100 rows 22.5, 30.0); then a CTA a row (197 rows 30.8 us in one, 39.9 in
+  // two: 3.9 TB/s; 256 rows 33.3: 4.7 TB/s).
+  const int vectors = (int)((x->vocab + 16 / el - 1) / (16 / el)), most = x->rows <= 8 ? 8 : (x->rows <= 74 ? 4 : 1);
   while (a.cluster < most && vectors >= 8192 * a.cluster) a.cluster *= 2;
   const bool vector = aligned(x->logits, 16) && (x->row_stride * (int64_t)el) % 16 == 0;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
