@@ -54,7 +54,7 @@ struct Few {
   static_assert(kWarps * W * (kRowF + 2) * 4 <= kRing, "rows of the four warps");
   static constexpr int kMeta = kRing;                              // [warp][stage] (scale of K, scale of V)
   static constexpr int kBefore = kMeta + kWarps * kStages * 8;     // units ahead of each sequence
-  static int bytes(int n_seqs) { return kBefore + 8 * (n_seqs + 1); }
+  static int bytes(int n_seqs) { return kBefore + 8 * (n_seqs + 1 + kCutWords); }
 };
 
 // Places of a 16-byte piece c of row r: keys are read by quads of lanes, eight rows side by side; values by eight lanes of one
@@ -70,21 +70,20 @@ __global__ void __launch_bounds__(kThreads) cache_attention_few_kernel(const __g
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, q4 = lane & 3;
   long long* before = reinterpret_cast<long long*>(smem + F::kBefore);
   pdl_launch_dependents();
-  const long long units = count_units<W>(a, before);
-  const AttnRuns runs(a, units, (int)gridDim.x);
+  const AttnRuns runs = cut_units<W>(a, before, (int)gridDim.x);
   const int cta = (int)blockIdx.x;
   if (tid == 0) a.joins[cta] = make_int4(0, 0, 0, 0);
-  if (cta >= runs.n_ctas || units == 0) return;
+  if (cta >= runs.n_ctas || runs.units == 0) return;
   const long long u_begin = runs.begin(cta), u_end = runs.begin(cta + 1);
   const uint32_t ring = smem_u32(smem) + (uint32_t)(warp * F::kStages * F::kStage);
   float2* meta = reinterpret_cast<float2*>(smem + F::kMeta) + warp * F::kStages;
 
   for (long long u = u_begin; u < u_end;) {
-    const AttnItem it = item_at<W>(a, before, u, u_end);
+    const AttnItem it = item_at<W>(a, before, runs, u, u_end);
     if (it.n < 1) break;
     const SeqShape& s = it.s;
     const int r0 = it.r0, n_cols = it.n_cols;
-    u += it.n;
+    u += it.span;
 
     // ---- pages on their way: step i of the item, the warp's half of one of its two pages ----------------------------
     int id = -1;                     // page (of the 32 that the step being loaded is among) lane `lane`, and its scales
@@ -353,7 +352,7 @@ __global__ void __launch_bounds__(kThreads) cache_attention_few_kernel(const __g
       }
     }
     if (begun && !goes_on && tid == 0) {
-      a.joins[cta] = make_int4(1 + runs.cta_of(u - it.of), s.first, r0, it.head | (n_cols << 16));
+      a.joins[cta] = make_int4(1 + runs.cta_of(u - it.span - (it.page - it.first)), s.first, r0, it.head | (n_cols << 16));
     }
   }
 }
@@ -361,11 +360,47 @@ __global__ void __launch_bounds__(kThreads) cache_attention_few_kernel(const __g
 // ---- rows that several CTAs worked on ------------------------------------------------------------------------------
 constexpr int kJoinWarps = 8, kJoinThreads = 32 * kJoinWarps, kJoinBlocks = 4 * 148;
 struct JoinShared {
-  int list[kFewCtas], count[(kFewCtas + 31) / 32];
+  int4 list[kFewCtas];                  // what the last CTA of an item noted
+  int last[kFewCtas], count[(kFewCtas + 31) / 32];
   float2 st[kJoinWarps];
   float4 o[kJoinWarps][32];
 };
-// A part of a row: a lane four dims of it
+// Parts of a row, up to 32 side by side: a lane knows one's reference and sum (on: there is one), and has four dims of each, which `get` gives
+// for any of them.  m, l: of all of them, in every lane; o: the lane's dims relative to m.
+template <typename Get>
+__device__ __forceinline__ void join_parts(int n, bool on, float2 st, float& m, float& l, float4& o, Get get) {
+  constexpr int U = 8;                                     // on their way at a time
+  float4 v[U];
+#pragma unroll
+  for (int i = 0; i < U; ++i) v[i] = i < n ? get(i) : make_float4(0.f, 0.f, 0.f, 0.f);
+  on = on && st.x != -INFINITY;
+  float top = on ? st.x : -INFINITY;
+#pragma unroll
+  for (int k = 16; k > 0; k >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, k));
+  top = fmaxf(top, m);
+  const float f = on ? exp2f(st.x - top) : -1.f;           // (-1: nothing there)
+  float sum = on ? times_power(st.y, st.x - top) : 0.f;
+#pragma unroll
+  for (int k = 16; k > 0; k >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, k);
+  if (m != -INFINITY) {
+    const float r = exp2f(m - top);
+    o.x *= r; o.y *= r; o.z *= r; o.w *= r;
+    sum += times_power(l, m - top);
+  }
+  l = sum;
+  m = top;
+#pragma unroll 1
+  for (int c = 0; c < n; c += U) {
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const float fi = __shfl_sync(0xffffffffu, f, c + i);
+      if (c + i < n && fi != -1.f) { o.x = fmaf(fi, v[i].x, o.x); o.y = fmaf(fi, v[i].y, o.y); o.z = fmaf(fi, v[i].z, o.z); o.w = fmaf(fi, v[i].w, o.w); }
+    }
+#pragma unroll
+    for (int i = 0; i < U; ++i) v[i] = c + U + i < n ? get(c + U + i) : make_float4(0.f, 0.f, 0.f, 0.f);
+  }
+}
+// one more part of a row: a lane four dims of it
 struct Sum { float m, l; float4 o; };
 __device__ __forceinline__ void add_part(Sum& s, float2 st, float4 v) {
   if (st.x == -INFINITY) return;
@@ -382,10 +417,12 @@ __device__ __forceinline__ void join_items(const CacheAttnArgs& a, const int4* j
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   // (in the order of the CTAs: the same list in every block)
   unsigned set[PER];
+  int4 note[PER];
 #pragma unroll
   for (int k = 0; k < PER; ++k) {
     const int chunk = warp + kJoinWarps * k, c = 32 * chunk + lane;
-    set[k] = __ballot_sync(0xffffffffu, c < ctas && joins[min(c, ctas - 1)].x != 0);
+    note[k] = joins[min(c, ctas - 1)];
+    set[k] = __ballot_sync(0xffffffffu, c < ctas && note[k].x != 0);
     if (lane == 0 && chunk < CHUNKS) sm.count[chunk] = __popc(set[k]);
   }
   __syncthreads();
@@ -396,52 +433,82 @@ __device__ __forceinline__ void join_items(const CacheAttnArgs& a, const int4* j
     const int chunk = warp + kJoinWarps * k;
     int at = __popc(set[k] & ((1u << lane) - 1u));
     for (int i = 0; i < min(chunk, CHUNKS); ++i) at += sm.count[i];
-    if ((set[k] >> lane) & 1u) sm.list[at] = 32 * chunk + lane;
+    if ((set[k] >> lane) & 1u) { sm.list[at] = note[k]; sm.last[at] = 32 * chunk + lane; }
   }
   __syncthreads();
-  const bool wide = W >= 8 * kJoinWarps && listed * (W / kJoinWarps) >= (int)gridDim.x;
-  const int groups = wide ? W / kJoinWarps : W, step = wide ? 1 : kJoinWarps;
-  for (int at = (int)blockIdx.x; at < listed * groups; at += (int)gridDim.x) {
-    const int last = sm.list[at / groups], col = wide ? (at % groups) * kJoinWarps + warp : at % groups;
-    const int4 j = joins[last];
-    const int first = j.x - 1;
-    const bool on = col < (j.w >> 16);                      // (the whole warp; without `wide` the whole block)
-    Sum s = {-INFINITY, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
-    constexpr int U = 4;
-    for (int c0 = first + (wide ? 0 : warp); c0 <= last && on; c0 += U * step) {
-      float2 st[U];
-      float4 v[U];
-#pragma unroll
-      for (int i = 0; i < U; ++i) {
-        const int c = c0 + i * step, place = c == first ? 1 : 0;
-        st[i] = make_float2(-INFINITY, 0.f);
-        v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (c <= last) {
-          st[i] = part_stats<W, D>(parts, c, place)[col];
-          if (lane < D / 4) v[i] = *reinterpret_cast<const float4*>(part_rows<W, D>(parts, c, place) + (size_t)col * D + 4 * lane);
-        }
-      }
-#pragma unroll
-      for (int i = 0; i < U; ++i) add_part(s, st[i], v[i]);
-    }
-    if (!wide) {
-      __syncthreads();                                      // (the round before has been read)
-      if (lane == 0) sm.st[warp] = make_float2(s.m, s.l);
-      sm.o[warp][lane] = s.o;
-      __syncthreads();
-      if (warp != 0) continue;
-      for (int w = 1; w < kJoinWarps; ++w) add_part(s, sm.st[w], sm.o[w][lane]);
-    }
-    if (!on) continue;
-    const float inv = s.l == 0.f ? 0.f : 1.f / s.l;
+  auto finish = [&](const int4& j, int col, float m, float l, const float4& o) {
+    const float inv = l == 0.f ? 0.f : 1.f / l;
     const RowHead to = row_head(a, j.y, j.z + col, j.w & 0xffff);
-    if (lane < D / 4) store_row_piece(a, to, 4 * lane, make_float4(s.o.x * inv, s.o.y * inv, s.o.z * inv, s.o.w * inv));
-    if (lane == 0) store_lse(a, to, s.m, s.l);
+    if (lane < D / 4) store_row_piece(a, to, 4 * lane, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
+    if (lane == 0) store_lse(a, to, m, l);
+  };
+  if constexpr (W >= 8 * kJoinWarps) {
+    constexpr int P = 1, U = 4, groups = W / (P * kJoinWarps);          // columns of a warp, parts on their way at a time
+    if (listed * groups >= (int)gridDim.x) {
+      for (int at = (int)blockIdx.x; at < listed * groups; at += (int)gridDim.x) {
+        const int item = at / groups, col0 = (at % groups) * (P * kJoinWarps) + warp * P;
+        const int4 j = sm.list[item];
+        const int first = j.x - 1, last = sm.last[item];
+        if (col0 >= (j.w >> 16)) continue;                  // (the whole warp)
+        Sum s[P];
+#pragma unroll
+        for (int p = 0; p < P; ++p) s[p] = {-INFINITY, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
+#pragma unroll 1
+        for (int c0 = first; c0 <= last; c0 += U) {
+          float2 st[U][P];
+          float4 v[U][P];
+#pragma unroll
+          for (int i = 0; i < U; ++i)
+#pragma unroll
+            for (int p = 0; p < P; ++p) {
+              const int c = min(c0 + i, last), place = c == first ? 1 : 0;
+              st[i][p] = c0 + i <= last ? part_stats<W, D>(parts, c, place)[col0 + p] : make_float2(-INFINITY, 0.f);
+              v[i][p] = c0 + i <= last && lane < D / 4 ? *reinterpret_cast<const float4*>(part_rows<W, D>(parts, c, place) + (size_t)(col0 + p) * D + 4 * lane)
+                                                       : make_float4(0.f, 0.f, 0.f, 0.f);
+            }
+#pragma unroll
+          for (int i = 0; i < U; ++i)
+#pragma unroll
+            for (int p = 0; p < P; ++p) add_part(s[p], st[i][p], v[i][p]);
+        }
+#pragma unroll
+        for (int p = 0; p < P; ++p) if (col0 + p < (j.w >> 16)) finish(j, col0 + p, s[p].m, s[p].l, s[p].o);
+      }
+      return;
+    }
+  }
+  for (int at = (int)blockIdx.x; at < listed * W; at += (int)gridDim.x) {
+    const int item = at / W, col = at % W;
+    const int4 j = sm.list[item];
+    const int first = j.x - 1, last = sm.last[item];
+    if (col >= (j.w >> 16)) continue;                      // (the whole block)
+    float m = -INFINITY, l = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+    for (int c0 = first + warp; c0 <= last; c0 += 32 * kJoinWarps) {
+      const int n = min(32, (last - c0) / kJoinWarps + 1);
+      auto place = [&](int c) { return c == first ? 1 : 0; };
+      const int mine = c0 + min(lane, n - 1) * kJoinWarps;
+      const float2 st = part_stats<W, D>(parts, mine, place(mine))[col];
+      join_parts(n, lane < n, st, m, l, o, [&](int i) {
+        const int c = c0 + i * kJoinWarps;
+        return lane < D / 4 ? *reinterpret_cast<const float4*>(part_rows<W, D>(parts, c, place(c)) + (size_t)col * D + 4 * lane) : make_float4(0.f, 0.f, 0.f, 0.f);
+      });
+    }
+    __syncthreads();                                        // (the round before has been read)
+    if (lane == 0) sm.st[warp] = make_float2(m, l);
+    sm.o[warp][lane] = o;
+    __syncthreads();
+    if (warp != 0) continue;
+    m = -INFINITY;
+    o = make_float4(0.f, 0.f, 0.f, 0.f);
+    join_parts(kJoinWarps, lane < kJoinWarps, sm.st[lane & (kJoinWarps - 1)], m, l, o, [&](int i) { return sm.o[i][lane]; });
+    finish(j, col, m, l, o);
   }
 }
 struct Parts { int4* joins; float* parts; };
 template <int D, int WF, bool kMany>
-__global__ void __launch_bounds__(kJoinThreads) cache_attention_join_kernel(const __grid_constant__ CacheAttnArgs a, Parts few, Parts many) {
+__global__ void __launch_bounds__(kJoinThreads, kJoinBlocks / 148) cache_attention_join_kernel(const __grid_constant__ CacheAttnArgs a, Parts few, Parts many) {
   __shared__ JoinShared sm;
   pdl_wait();
   if constexpr (WF > 0) join_items<WF, D>(a, few.joins, few.parts, kFewCtas, sm);

@@ -62,43 +62,16 @@ __device__ __forceinline__ PageRange pages_of(const CacheAttnArgs& a, const SeqS
   return {first, max((keys_of(a, s, min(by_group(a, tile * W + W - 1), s.n - 1)).hi + kPage - 1) / kPage - first, 1)};
 }
 
-// The units (item, page) of all sequences lie end to end and are cut into equal runs, one a CTA.  `before` (shared memory, n_seqs + 1):
-// units of the sequences ahead of each.  Called by the whole block; ends with a barrier.
-template <int W>
-__device__ __forceinline__ long long count_units(const CacheAttnArgs& a, long long* before) {
-  if (threadIdx.x < 32) {
-    const int lane = threadIdx.x;
-    long long ahead = 0;
-    for (int base = 0; base < a.r.n_seqs; base += 32) {
-      const int i = base + lane;
-      long long u = 0;
-      if (i < a.r.n_seqs) {
-        const SeqShape s = shape_of<W>(a, i);
-#pragma unroll 1
-        for (int tile = 0; tile < s.tiles; ++tile) u += pages_of<W>(a, s, tile).n;
-        u *= a.c.n_kv_heads;
-      }
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) { const long long t = __shfl_up_sync(0xffffffffu, u, o); if (lane >= o) u += t; }
-      if (i < a.r.n_seqs) before[i + 1] = ahead + u;
-      ahead += __shfl_sync(0xffffffffu, u, 31);
-    }
-    if (lane == 0) before[0] = 0;
-  }
-  __syncthreads();
-  return before[a.r.n_seqs];
-}
 __device__ __forceinline__ long long divide(long long x, long long y) { return ((x | y) >> 31) == 0 ? (long long)((uint32_t)x / (uint32_t)y) : x / y; }
-// The runs: n_ctas of `each` units, the first `longer` of them of one more.
+__device__ __forceinline__ int rounded_up(int x, int to) { return to <= 1 ? x : (x + to - 1) / to * to; }
+
+// The units (item, page) of all sequences lie end to end and are cut into equal runs, one a CTA: n_ctas of `each` units, the first `longer` of them
+// of one more.  A run that crosses from one item to the next pays for both a beginning and an end twice, about what four pages take.  So where
+// it costs no more than three pages a CTA, each item is counted as a whole number of runs and none crosses (one row over 211
+// pages, four heads: 13.1 us from first to last, of which two CTAs that crossed took 3.5).
 struct AttnRuns {
-  long long each;
-  int n_ctas, longer;
-  __device__ __forceinline__ AttnRuns(const CacheAttnArgs& a, long long units, int grid) {
-    n_ctas = (int)min((long long)grid, (units + (1 << a.page_shift) - 1) >> a.page_shift);
-    n_ctas = max(n_ctas, 1);
-    each = divide(units, n_ctas);
-    longer = (int)(units - each * n_ctas);
-  }
+  long long units, each;
+  int n_ctas, longer, whole;           // whole: units that an item is rounded up to (0: they are as they are)
   __device__ __forceinline__ long long begin(int cta) const { return each * cta + min(cta, longer); }
   // the CTA whose run holds `unit`
   __device__ __forceinline__ int cta_of(long long unit) const {
@@ -106,11 +79,67 @@ struct AttnRuns {
     return unit < head ? (int)divide(unit, each + 1) : longer + (int)divide(unit - head, each);
   }
 };
-
-// An item's pages that this CTA works on: [page, page + n) of the pages [first, first + of).
-struct AttnItem { SeqShape s; int seq, r0, n_cols, head, page, n, first, of; };
+// `before` (shared memory, n_seqs + 1 numbers and kCutWords): units of the sequences ahead of each; how the units are cut.  Called by the
+// whole block; ends with a barrier.
+constexpr int kCutWords = 3;
 template <int W>
-__device__ __forceinline__ AttnItem item_at(const CacheAttnArgs& a, const long long* before, long long unit, long long end) {
+__device__ __forceinline__ AttnRuns cut_units(const CacheAttnArgs& a, long long* before, int grid) {
+  if (threadIdx.x < 32) {
+    const int lane = threadIdx.x, least = 1 << a.page_shift;
+    auto units_of = [&](int i, int whole, int& items) {
+      const SeqShape s = shape_of<W>(a, i);
+      long long u = 0;
+#pragma unroll 1
+      for (int tile = 0; tile < s.tiles; ++tile) u += rounded_up(pages_of<W>(a, s, tile).n, whole);
+      items += min(s.tiles, grid) * a.c.n_kv_heads;
+      return u * a.c.n_kv_heads;
+    };
+    // all units and items, as far as the rule asks for them
+    uint32_t units = 0u;
+    int items = 0, whole = 0;
+#pragma unroll 1
+    for (int i = lane; i < a.r.n_seqs; i += 32) units = min(units + (uint32_t)min(units_of(i, 0, items), 1ll << 24), 1u << 24);
+    units = __reduce_add_sync(0xffffffffu, units);
+    items = __reduce_add_sync(0xffffffffu, min(items, grid));
+    if (units < (1u << 24) && 2 * items <= grid) {
+      const int rounded = max((int)(units + grid - items - 1) / (grid - items), least), equal = max((int)(units + grid - 1) / grid, least);
+      if (rounded - equal <= 3) whole = rounded;
+    }
+    long long ahead = 0;
+#pragma unroll 1
+    for (int base = 0; base < a.r.n_seqs; base += 32) {
+      const int i = base + lane;
+      long long u = i < a.r.n_seqs ? units_of(i, whole, items) : 0;
+      if (a.r.n_seqs > 1) {
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) { const long long t = __shfl_up_sync(0xffffffffu, u, o); if (lane >= o) u += t; }
+      }
+      if (i < a.r.n_seqs) before[i + 1] = ahead + u;
+      ahead += __shfl_sync(0xffffffffu, u, a.r.n_seqs > 1 ? 31 : 0);
+    }
+    if (lane == 0) {
+      const int n = whole > 0 ? max((int)ahead / whole, 1) : max((int)min((long long)grid, (ahead + least - 1) >> a.page_shift), 1);
+      const long long each = whole > 0 ? whole : divide(ahead, n);
+      before[0] = 0;
+      before[a.r.n_seqs + 1] = each;
+      before[a.r.n_seqs + 2] = n | (whole > 0 ? 0 : (ahead - each * n) << 32);
+      before[a.r.n_seqs + 3] = whole;
+    }
+  }
+  __syncthreads();
+  AttnRuns c;
+  c.units = before[a.r.n_seqs];
+  c.each = before[a.r.n_seqs + 1];
+  c.n_ctas = (int)before[a.r.n_seqs + 2];
+  c.longer = (int)(before[a.r.n_seqs + 2] >> 32);
+  c.whole = (int)before[a.r.n_seqs + 3];
+  return c;
+}
+
+// An item's pages that this CTA works on: [page, page + n) of the pages [first, first + of); `span` units of its run.
+struct AttnItem { SeqShape s; int seq, r0, n_cols, head, page, n, first, of; long long span; };
+template <int W>
+__device__ __forceinline__ AttnItem item_at(const CacheAttnArgs& a, const long long* before, const AttnRuns& runs, long long unit, long long end) {
   int lo = 0;
   if (a.r.n_seqs > 1) {
     int hi = a.r.n_seqs - 1;
@@ -124,15 +153,17 @@ __device__ __forceinline__ AttnItem item_at(const CacheAttnArgs& a, const long l
 #pragma unroll 1
   for (int tile = 0; tile < it.s.tiles; ++tile) {
     const PageRange p = pages_of<W>(a, it.s, tile);
-    const long long here = (long long)p.n * a.c.n_kv_heads;
+    const int of = rounded_up(p.n, runs.whole);
+    const long long here = (long long)of * a.c.n_kv_heads;
     if (u < here) {
       it.r0 = tile * W;
       it.n_cols = min(W, it.s.n * a.G - it.r0);
       int head = 0;
-      while (u >= p.n) { u -= p.n; ++head; }
+      while (u >= of) { u -= of; ++head; }
       it.head = head;
       it.page = p.first + (int)u;
-      it.n = (int)min((long long)p.n - u, end - unit);
+      it.span = min((long long)of - u, end - unit);
+      it.n = (int)min((long long)p.n - u, it.span);
       it.first = p.first;
       it.of = p.n;
       break;

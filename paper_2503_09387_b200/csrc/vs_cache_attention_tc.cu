@@ -41,7 +41,7 @@ struct Tc {
   static constexpr int kFlags = kCtl + 8 * kBars;       // [place] first and end of the rows of the raw tile that count (end 0: the page is not there)
   static constexpr int kSlotWord = kFlags + 8 * kRing;
   static constexpr int kBefore = (kSlotWord + 8 + 7) / 8 * 8;
-  static int bytes(int n_seqs) { return kBefore + 8 * (n_seqs + 1); }
+  static int bytes(int n_seqs) { return kBefore + 8 * (n_seqs + 1 + kCutWords); }
 };
 
 // The page tiles of an item of n pages in the order of their use: K(0), K(1), V(0), K(2), V(1), ... K(n - 1), V(n - 2), V(n - 1)
@@ -136,13 +136,12 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attention_tc_kernel(const _
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   tc_fence_before();
-  const long long units = count_units<kWide>(a, before);           // (ends with a barrier of the block)
+  const AttnRuns runs = cut_units<kWide>(a, before, (int)gridDim.x);         // (ends with a barrier of the block)
   tc_fence_after();
   const uint32_t tmem = *tmem_slot, tmem_o = tmem + kTiles * 128u;
-  const AttnRuns runs(a, units, (int)gridDim.x);
   const int cta = (int)blockIdx.x;
   if (tid == 0) a.joins[cta] = make_int4(0, 0, 0, 0);
-  const bool works = cta < runs.n_ctas && units > 0;
+  const bool works = cta < runs.n_ctas && runs.units > 0;
   const long long u_begin = works ? runs.begin(cta) : 0, u_end = works ? runs.begin(cta + 1) : 0;
 
   if (warp >= kLoaderWarp) {
@@ -152,9 +151,9 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attention_tc_kernel(const _
       uint32_t done = 0;                                                   // tiles of the items so far
       bool ok = true;
       for (long long u = u_begin; u < u_end && ok;) {
-        const AttnItem it = item_at<kWide>(a, before, u, u_end);
+        const AttnItem it = item_at<kWide>(a, before, runs, u, u_end);
         if (it.n < 1) break;
-        u += it.n;
+        u += it.span;
         // keys that any row of the item sees
         const int lo = keys_of(a, it.s, by_group(a, it.r0)).lo, hi = keys_of(a, it.s, by_group(a, it.r0 + it.n_cols - 1)).hi;
         uint32_t place = (done + (uint32_t)lane) % kRing, phase = ((done + (uint32_t)lane) / kRing + 1u) & 1u;      // (phase: of bar_raw_free, before this use)
@@ -204,9 +203,9 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attention_tc_kernel(const _
       uint32_t done = 0, g = 0, n_items = 0;                               // page tiles of the items so far; pages and items of the row tile
       bool ok = true;
       for (long long u = u_begin; u < u_end && ok;) {
-        const AttnItem it = item_at<kWide>(a, before, u, u_end);
+        const AttnItem it = item_at<kWide>(a, before, runs, u, u_end);
         if (it.n < 1) break;
-        u += it.n;
+        u += it.span;
         const bool mine = it.n_cols > i * kRows;                           // (else the page tiles are only let go)
         auto wait_tile = [&](int e) { const uint32_t x = done + (uint32_t)e; return wait_all(bar_full(x % kRing), (x / kRing) & 1u); };
         auto tile_at = [&](int e) { return base + L::kF16 + ((done + (uint32_t)e) % kRing) * (uint32_t)L::kTile; };
@@ -274,9 +273,9 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attention_tc_kernel(const _
     uint32_t end = 0, x = half;                                            // page tiles to the end of the item; the tile at hand
     bool ok = true;
     for (long long u = u_begin; u < u_end && ok;) {
-      const AttnItem it = item_at<kWide>(a, before, u, u_end);
+      const AttnItem it = item_at<kWide>(a, before, runs, u, u_end);
       if (it.n < 1) break;
-      u += it.n;
+      u += it.span;
       end += 2u * (uint32_t)it.n;
 #pragma unroll 1
       for (; x < end; x += 2u) {
@@ -324,9 +323,9 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attention_tc_kernel(const _
     uint32_t g = 0;                                                        // pages so far
     bool ok = true;
     for (long long u = u_begin; u < u_end && ok;) {
-      const AttnItem it = item_at<kWide>(a, before, u, u_end);
+      const AttnItem it = item_at<kWide>(a, before, runs, u, u_end);
       if (it.n < 1) break;
-      u += it.n;
+      u += it.span;
       const int col = i * kRows + row;                                     // packed row of the item
       const bool on = col < it.n_cols;
       if (i * kRows >= it.n_cols) continue;                                // (no second tile)
@@ -522,7 +521,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attention_tc_kernel(const _
         }
       }
       tc_fence_before();
-      if (begun && !goes_on && tid == 0) a.joins[cta] = make_int4(1 + runs.cta_of(u - it.of), it.s.first, it.r0, it.head | (it.n_cols << 16));
+      if (begun && !goes_on && tid == 0) a.joins[cta] = make_int4(1 + runs.cta_of(u - it.span - (it.page - it.first)), it.s.first, it.r0, it.head | (it.n_cols << 16));
     }
     if (!ok) *abort_flag = 1;
   }
@@ -538,7 +537,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attention_tc_kernel(const _
 template <int D>
 int launch_tc(const CacheAttnArgs& a, bool behind_few, cudaStream_t st) {
   const int bytes = Tc<D>::bytes(a.r.n_seqs);
-  static_assert(Tc<D>::kBefore + 8 * (VS_CACHE_MAX_SEQS + 1) <= 227 * 1024, "shared memory of an SM");
+  static_assert(Tc<D>::kBefore + 8 * (VS_CACHE_MAX_SEQS + 1 + kCutWords) <= 227 * 1024, "shared memory of an SM");
   if (cudaFuncSetAttribute(cache_attention_tc_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return VS_ERR_CUDA;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(kManyCtas);
