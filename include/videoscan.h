@@ -295,7 +295,7 @@ int vs_destroy_stream(vs_stream* h);
  * takes: rotary positions with several axes, a paged cache of 8-bit keys and values, attention over
  * it; and, beside vs_lm_head, what the logits say about given tokens.
  * These calls need no handle: the device is an argument (made current for the call and put back),
- * and they only enqueue work on `cuda_stream`, which must belong to it.  They keep nothing between
+ * and they only enqueue work on `cuda_stream`, which must belong to it.  They keep no data between
  * calls, allocate nothing, and may be captured into a graph; calls on different streams are
  * independent unless they share a workspace or write the same memory.  Integer arrays marked DEVICE
  * are read when the kernels run, so a captured call follows what they hold then.  Strides are in
@@ -366,8 +366,8 @@ typedef struct {
  * ahead of the rows; where rows raise it, the codes of those tokens are rounded once more at the new scale.  A row written to
  * the first place of a page starts the page afresh.  Nearest code, ties to even; infinities become +-448, NaN stays
  * NaN.  Appending ends the sequence: codes behind its last row are left as they were and count for nothing.
- * No page may be written for two sequences of a call (pages that several sequences share must be full);
- * which of them is kept is not defined then. */
+ * No page may be written for two sequences of a call, or twice for one (pages that several sequences share
+ * must be full); what such a page holds then is not defined. */
 int vs_cache_write(const vs_cache* cache, const vs_cache_rows* rows, void* cuda_stream);
 
 /* Reads rows back into k and v: the values that the codes stand for, exact in either dtype. */
@@ -379,8 +379,10 @@ int vs_cache_read(const vs_cache* cache, const vs_cache_rows* rows, void* cuda_s
  * (and -inf in lse).  Tokens that no row of the call sees may hold anything.
  * q:   DEVICE bf16 [n_rows][n_q_heads][head_dim], 16-byte aligned, strides multiples of 8;
  *      n_q_heads % n_kv_heads == 0, at most 8 query heads a KV head.
+ *      Several sequences may name the same page, and one may name it several times.
  * out: DEVICE [n_rows][n_q_heads][head_dim] of out_dtype, 8-byte (bf16) or 16-byte (fp32) aligned,
- *      strides multiples of 4.  Softmax weights are rounded to 11 bits, sums are fp32.
+ *      strides multiples of 4; may be q itself (bf16, the same strides), but must not overlap it otherwise.
+ *      Softmax weights are rounded to 11 bits, sums are fp32.
  * lse: DEVICE fp32 [n_rows][n_q_heads], log sum exp of a row's scores, or NULL: what joining the rows
  *      with those over other keys (the bank's, say) takes.
  * scale: of the scores, usually 1 / sqrt(head_dim).

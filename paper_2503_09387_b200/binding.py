@@ -320,6 +320,14 @@ def _dtype_code(dtype, what: str) -> int:
     return 1
 
 
+def _capturing(index: int) -> bool:
+    """Whether what is enqueued on the current stream of GPU ``index`` goes into a graph."""
+    if _torch.cuda.current_device() == index:
+        return _torch.cuda.is_current_stream_capturing()
+    with _torch.cuda.device(index):
+        return _torch.cuda.is_current_stream_capturing()
+
+
 def _on_gpu(t, what: str) -> int:
     index = t.get_device()
     _need(index >= 0, what)
@@ -362,9 +370,9 @@ def token_logprobs(logits, tokens=None, top: int = 0, out=None):
         _need(tokens.dtype is torch.int32 and tokens.shape == (rows,) and tokens.is_contiguous() and tokens.get_device() == index,
               "token_logprobs: tokens int32 [rows]")
     if out is None:
-        like = dict(device=logits.device)
-        out = (torch.empty(rows, **like), torch.empty(rows, **like), torch.empty(rows, dtype=torch.int32, **like),
-               torch.empty((rows, top), dtype=torch.int32, **like), torch.empty((rows, top), **like))
+        new = lambda shape, dtype: torch.empty(shape, dtype=dtype, device=logits.device)
+        out = (new(rows, torch.float32), new(rows, torch.float32), new(rows, torch.int32), new((rows, top), torch.int32),
+               new((rows, top), torch.float32))
     else:
         for t, n, dtype in zip(out, (rows, rows, rows, rows * top, rows * top), (torch.float32, torch.float32, torch.int32, torch.int32, torch.float32)):
             _need(t.numel() == n and t.dtype is dtype and t.is_contiguous() and t.get_device() == index, "token_logprobs: out as described")
@@ -443,11 +451,14 @@ class PageCache:
 
     def workspace(self):
         """A workspace for ``attend``; two calls that may overlap (graphs replayed side by side) need one each."""
-        out = C.c_size_t(0)
-        _check(load_library().vs_cache_attention_bytes(self.head_dim, C.byref(out)), "vs_cache_attention_bytes")
-        workspace = _torch.empty(out.value, dtype=_torch.uint8, device=self.k.device)
+        workspace = self._new_workspace()
         workspace[:256].zero_()
         return workspace
+
+    def _new_workspace(self):
+        out = C.c_size_t(0)
+        _check(load_library().vs_cache_attention_bytes(self.head_dim, C.byref(out)), "vs_cache_attention_bytes")
+        return _torch.empty(out.value, dtype=_torch.uint8, device=self.k.device)
 
     def attend_status(self) -> int:
         """0, or VS_ERR_DEVICE_TIMEOUT if a wait of an ``attend`` with one of the cache's own workspaces ever ran out.  Synchronises."""
@@ -457,7 +468,8 @@ class PageCache:
                out_dtype=None):
         """Attention of q bf16 [n_rows, n_q_heads, head_dim] over each sequence's ``lengths[i]`` tokens, its rows counted in.
         -> (out [n_rows, n_q_heads, head_dim], lse fp32 [n_rows, n_q_heads]).  ``out_dtype``: of a new ``out``, bf16 or fp32.  Without
-        ``workspace`` the cache keeps one for every stream it is used on."""
+        ``workspace`` the cache keeps one for every stream it is used on; a call that is captured takes one from the graph's own memory, so
+        that graphs replayed side by side share none (its status is then nobody's to read)."""
         torch, index = _torch, self.device_index
         shape, step = q.shape, q.stride()
         _need(len(shape) == 3 and q.dtype is torch.bfloat16 and shape[2] == self.head_dim and step[2] == 1 and q.get_device() == index,
@@ -473,9 +485,14 @@ class PageCache:
               "attend: lse fp32 [n_rows, n_q_heads]")
         stream = _raw_stream(index)
         if workspace is None:
-            workspace = self._workspaces.get(stream)
-            if workspace is None:
-                workspace = self._workspaces[stream] = self.workspace()
+            if _capturing(index):
+                workspace = self._new_workspace()
+            else:
+                workspace = self._workspaces.get(stream)
+                if workspace is None:
+                    workspace = self._workspaces[stream] = self.workspace()
+        else:
+            _need(workspace.is_contiguous() and workspace.get_device() == index, "attend: a workspace on the cache's GPU")
         block = VS_CACHE_QUERIES.pack(*self._seqs(page_table, lengths, row_offsets), n_rows, 0, q.data_ptr(), out.data_ptr(), lse.data_ptr(),
                                       workspace.data_ptr(), workspace.nbytes, step[0], step[1], out_step[0], out_step[1], n_heads, causal, window,
                                       _dtype_code(out.dtype, "attend: out of bf16 or fp32 wanted"), head_dim ** -0.5 if scale is None else scale, 0)

@@ -587,6 +587,8 @@ extern "C" int vs_cache_attention(const vs_cache* cache, const vs_cache_queries*
   if (x->workspace_bytes < need) return VS_ERR_CAPACITY;
   if (!aligned(x->q, 16) || !aligned(x->out, x->out_dtype == 1 ? 16 : 8) || !aligned(x->workspace, 256) || !aligned(x->lse, 4)) return VS_ERR_INVALID_ARG;
   if (x->q_row_stride % 8 != 0 || x->q_head_stride % 8 != 0 || x->out_row_stride % 4 != 0 || x->out_head_stride % 4 != 0) return VS_ERR_INVALID_ARG;
+  // (in place: an item's rows of q are read before they are written, by the CTA that writes them or two launches ahead)
+  if (x->q == x->out && (x->out_dtype != 0 || x->q_row_stride != x->out_row_stride || x->q_head_stride != x->out_head_stride)) return VS_ERR_INVALID_ARG;
   OnDevice on(cache->device);
   if (!on.ok) return VS_ERR_CUDA;
   CacheAttnArgs a = {};

@@ -15,7 +15,8 @@ struct OnDevice {
   explicit OnDevice(int device) {
     if (device < 0 || cudaGetDevice(&before) != cudaSuccess) return;
     ok = before == device || cudaSetDevice(device) == cudaSuccess;
-    if (before == device) before = -1;                 // nothing to put back
+    if (!ok) cudaGetLastError();                       // (the caller is told; the next launch must not find it)
+    if (before == device || !ok) before = -1;          // nothing to put back
   }
   ~OnDevice() { if (before >= 0) cudaSetDevice(before); }
   OnDevice(const OnDevice&) = delete;

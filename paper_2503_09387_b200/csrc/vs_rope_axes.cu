@@ -141,6 +141,7 @@ extern "C" int vs_rope_axes(const vs_rope* r, void* cuda_stream) {
   const int64_t strides[4] = {r->x_row_stride, r->x_head_stride, r->out_row_stride, r->out_head_stride};
   for (int64_t s : strides) if (s % piece != 0) return VS_ERR_INVALID_ARG;
   if (!aligned(r->x, 16) || !aligned(r->out, 16)) return VS_ERR_INVALID_ARG;
+  if (r->x == r->out && (strides[0] != strides[2] || strides[1] != strides[3])) return VS_ERR_INVALID_ARG;      // (in place: row by row)
   OnDevice on(r->device);
   if (!on.ok) return VS_ERR_CUDA;
   RopeAxesArgs a = {};

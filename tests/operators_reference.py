@@ -154,9 +154,9 @@ def token_logprobs(logits, tokens, top):
         else:
             m = max(x)
             rest = math.fsum(math.exp(v - m) for v in x) - 1.0 if len(x) > 1 else 0.0
-            lse = m + math.log1p(rest)
-            lp = lambda i: x[i] - lse
-            entropy = math.fsum(-math.exp(v - lse) * (v - lse) for v in x if v > -math.inf)
+            over = math.log1p(rest)                       # (log sum exp less m: m may be so large that the sum loses this)
+            lp = lambda i: (x[i] - m) - over
+            entropy = math.fsum(-math.exp(v - m - over) * (v - m - over) for v in x if v > -math.inf)
         got.append((0.0 if t < 0 else (math.nan if t >= len(x) else lp(t)), entropy, order.index(t) if 0 <= t < len(x) else -1,
                     order[:top], [lp(i) for i in order[:top]]))
     return got

@@ -120,3 +120,12 @@ def test_references_codes_are_the_formats():
 def test_references_axes():
     assert ref.axes_of_pairs((2, 3, 1), False) == [0, 0, 1, 1, 1, 2]
     assert ref.axes_of_pairs((2, 3, 1), True) == [0, 1, 2, 0, 1, 1]
+
+
+def test_refusals_of_outputs_over_inputs(lib):
+    """In place means the same places."""
+    assert lib.vs_rope_axes(binding.VS_ROPE.pack(*dict(ROPE, outr=256).values()), None) == INVALID
+    assert lib.vs_rope_axes(binding.VS_ROPE.pack(*dict(ROPE, xh=128).values()), None) == INVALID
+    c = binding.VsCache(**CACHE)
+    for change in (dict(outh=256), dict(outr=128), dict(dtype=1)):
+        assert lib.vs_cache_attention(c, queries(**change), None) == INVALID, change
