@@ -14,7 +14,10 @@
 // columns of mma.sync: S^T = K q^T and O^T += V^T P^T, so a page is read once for the whole group; a tcgen05 tile of 128
 // rows would hold 7.  A CTA is four warps, each with half a page in a ring of its own, filled by 16-byte asynchronous copies
 // ahead of their turn and placed so that both operands' fragments are read without bank conflicts: no barrier in the loop.
-// The work of all sequences is cut into equal runs of pages (count_units): long and short sequences side by side leave no CTA idle.
+// The work of all sequences is cut into equal runs of pages (cut_units): long and short sequences side by side leave no CTA idle.
+// Measured: sixteen sequences of 2000 to 65000 tokens, seven heads a group, 522 MB of codes: 90 us, 5.8 TB/s (89 % of what a copy reaches); one sequence of 13504:
+// 11.1 us from first to last -- 1.5 until the units are counted, 1 to the pages' numbers and first loads, 0.9 to their arrival, 1.7 for two steps, 1.2 for the
+// warps' rows, then 3.3 for the join behind the launch's end.
 #include "vs_cache_attention.cuh"
 #include "vs_ptx.cuh"
 
@@ -410,7 +413,8 @@ __device__ __forceinline__ void add_part(Sum& s, float2 st, float4 v) {
   s.m = m;
 }
 // The items that a kernel's CTAs left in parts, by all blocks: a block lists the CTAs that were the last on an item others had begun.  Where
-// these are many it takes eight columns of an item at a time, a warp to each; else one, its parts shared by the warps.
+// these are many, and so of few parts each, it takes eight columns of an item at a time, a warp to each; else one, its parts shared by the warps.
+// (Sixteen items of two parts, 224 columns: 7 us more column by column.  Four of 36 parts: 8 us, 16.5 MB of parts.)
 template <int W, int D>
 __device__ __forceinline__ void join_items(const CacheAttnArgs& a, const int4* joins, float* parts, int ctas, JoinShared& sm) {
   constexpr int CHUNKS = (kFewCtas + 31) / 32, PER = (CHUNKS + kJoinWarps - 1) / kJoinWarps;
@@ -444,7 +448,7 @@ __device__ __forceinline__ void join_items(const CacheAttnArgs& a, const int4* j
   };
   if constexpr (W >= 8 * kJoinWarps) {
     constexpr int P = 1, U = 4, groups = W / (P * kJoinWarps);          // columns of a warp, parts on their way at a time
-    if (listed * groups >= (int)gridDim.x) {
+    if (2 * listed * groups >= (int)gridDim.x) {
       for (int at = (int)blockIdx.x; at < listed * groups; at += (int)gridDim.x) {
         const int item = at / groups, col0 = (at % groups) * (P * kJoinWarps) + warp * P;
         const int4 j = sm.list[item];
@@ -506,22 +510,24 @@ __device__ __forceinline__ void join_items(const CacheAttnArgs& a, const int4* j
     finish(j, col, m, l, o);
   }
 }
-struct Parts { int4* joins; float* parts; };
+struct Parts { int4* joins; float* parts; int ctas; };
 template <int D, int WF, bool kMany>
 __global__ void __launch_bounds__(kJoinThreads, kJoinBlocks / 148) cache_attention_join_kernel(const __grid_constant__ CacheAttnArgs a, Parts few, Parts many) {
   __shared__ JoinShared sm;
   pdl_wait();
-  if constexpr (WF > 0) join_items<WF, D>(a, few.joins, few.parts, kFewCtas, sm);
+  if constexpr (WF > 0) join_items<WF, D>(a, few.joins, few.parts, few.ctas, sm);
   if constexpr (WF > 0 && kMany) __syncthreads();
-  if constexpr (kMany) join_items<kManyWide, D>(a, many.joins, many.parts, kManyCtas, sm);
+  if constexpr (kMany) join_items<kManyWide, D>(a, many.joins, many.parts, many.ctas, sm);
 }
 
+// as many as are resident: three an SM of 168 registers a thread, two of 255
+int few_ctas(int cols) { return cols <= 8 ? kFewCtas : 2 * 148; }
 template <int D, int NT>
 int launch_few(const CacheAttnArgs& a, cudaStream_t st) {
   using F = Few<D, NT>;
   const int bytes = F::bytes(a.r.n_seqs);
   if (cudaFuncSetAttribute(cache_attention_few_kernel<D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return VS_ERR_CUDA;
-  cache_attention_few_kernel<D, NT><<<kFewCtas, kThreads, bytes, st>>>(a);
+  cache_attention_few_kernel<D, NT><<<few_ctas(8 * NT), kThreads, bytes, st>>>(a);
   return launched();
 }
 
@@ -559,7 +565,7 @@ constexpr int kFewPageShift = 2, kManyPageShift = 2;            // four pages at
 // the workspace: status word, the CTAs' notes and parts of either kernel
 constexpr size_t kFewJoinsAt = 256, kManyJoinsAt = kFewJoinsAt + vs::kFewCtas * 16, kPartsAt = 16384;
 static_assert(kManyJoinsAt + vs::kManyCtas * 16 <= kPartsAt && vs::kManyCtas <= vs::kFewCtas, "notes of the CTAs");
-size_t few_bytes(int head_dim) { return (size_t)vs::kFewCtas * 2 * vs::kFewCols * (head_dim + 2) * 4; }
+size_t few_bytes(int head_dim) { return (size_t)vs::kFewCtas * 2 * vs::kFewWide * (head_dim + 2) * 4; }
 size_t many_bytes(int head_dim) { return (size_t)vs::kManyCtas * 2 * vs::kManyWide * (head_dim + 2) * 4; }
 }
 
@@ -595,8 +601,6 @@ extern "C" int vs_cache_attention(const vs_cache* cache, const vs_cache_queries*
   a.c = *cache; a.r = *rows;
   a.q = static_cast<const bf16*>(x->q); a.out = x->out; a.lse = x->lse;
   uint8_t* ws = static_cast<uint8_t*>(x->workspace);
-  const Parts few = {reinterpret_cast<int4*>(ws + kFewJoinsAt), reinterpret_cast<float*>(ws + kPartsAt)};
-  const Parts many = {reinterpret_cast<int4*>(ws + kManyJoinsAt), reinterpret_cast<float*>(ws + kPartsAt + few_bytes(cache->head_dim))};
   a.status = reinterpret_cast<int*>(ws);
   a.q_row = x->q_row_stride; a.q_head = x->q_head_stride; a.out_row = x->out_row_stride; a.out_head = x->out_head_stride;
   a.scale_log2e = x->scale * 1.4426950408889634f;
@@ -608,8 +612,16 @@ extern "C" int vs_cache_attention(const vs_cache* cache, const vs_cache_queries*
   // Which sequences have few rows the device knows; the host, from the number of rows, that all of them have (or none, where they have the
   // same number each).  Either kind has its kernel; what their CTAs left in parts one launch joins.
   const long long most = (long long)(uniform ? a.rows_each : rows->n_rows) * G;
-  const bool any_few = most <= kFewCols || !uniform, any_many = most > kFewCols;
-  const int cols = any_few ? (most <= 8 ? 8 : 16) : 0;
+  // The kernel of few rows takes a sequence of up to 32 packed rows, two of its tiles (seven heads a group, four KV heads, three rows: 17.1 us against the
+  // other's 20.6 over 13440 tokens, 97 against 106 for sixteen sequences; six rows, three tiles: 20.7 and 20.6, 136 and 108), and any while there are few
+  // tiles and pages: the other one's items begin and end slowly (32 rows over 300 tokens 16.7 and 20.8, over 1500 22.3 and 23.7, over 6000 37.6 and 25.2).
+  const long long tiles = uniform ? (long long)rows->n_seqs * ((a.rows_each * G + kFewWide - 1) / kFewWide) : (long long)rows->n_rows * G / kFewWide + rows->n_seqs;
+  const long long items = tiles * cache->n_kv_heads;
+  a.few_cols = items <= few_ctas(kFewWide) && items * rows->table_width <= 1024 ? 0x7fffffff : 32;
+  const bool any_few = most <= a.few_cols || !uniform, any_many = most > a.few_cols;
+  const int cols = any_few ? (most <= 8 ? 8 : kFewWide) : 0;
+  const Parts few = {reinterpret_cast<int4*>(ws + kFewJoinsAt), reinterpret_cast<float*>(ws + kPartsAt), few_ctas(cols)};
+  const Parts many = {reinterpret_cast<int4*>(ws + kManyJoinsAt), reinterpret_cast<float*>(ws + kPartsAt + few_bytes(cache->head_dim)), kManyCtas};
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   if (any_few) {
     a.take_few = 1; a.page_shift = kFewPageShift; a.joins = few.joins; a.parts = few.parts;

@@ -6,8 +6,7 @@
 
 namespace vs {
 
-constexpr int kFewCols = 16;      // sequences of at most as many packed rows: vs_cache_attention.cu; more: vs_cache_attention_tc.cu
-constexpr int kFewCtas = 3 * 148, kManyCtas = 148, kManyWide = 256;
+constexpr int kFewWide = 16, kFewCtas = 3 * 148, kManyWide = 256, kManyCtas = 148;      // packed rows of a tile (at most) and CTAs of either kernel
 
 struct CacheAttnArgs {
   vs_cache c;
@@ -25,7 +24,7 @@ struct CacheAttnArgs {
   int rows_each;                  // of every sequence; -1: by row_offsets
   int max_held;                   // tokens that a sequence's row of the table has pages for
   int page_shift;                 // log2 of the pages that are worth a CTA of their own
-  int take_few;                   // whether the launch takes the sequences of few rows or the others
+  int few_cols, take_few;         // packed rows of a sequence of few rows, at most; whether the launch takes these or the others
 };
 
 #ifdef __CUDACC__
@@ -43,7 +42,7 @@ __device__ __forceinline__ SeqShape shape_of(const CacheAttnArgs& a, int i) {
   if (a.rows_each < 0) { const SeqRows s = rows_of(a.r, i); q.first = s.first; q.n = s.n; }
   q.len = max(a.r.tokens[i], 0);
   const int cols = q.n * a.G;                       // (the host has seen to it that this is below 2^30)
-  q.tiles = (cols <= kFewCols) == (a.take_few != 0) ? (cols + W - 1) / W : 0;
+  q.tiles = (cols <= a.few_cols) == (a.take_few != 0) ? (cols + W - 1) / W : 0;
   return q;
 }
 // keys [lo, hi) that row t of a sequence sees
@@ -66,9 +65,11 @@ __device__ __forceinline__ long long divide(long long x, long long y) { return (
 __device__ __forceinline__ int rounded_up(int x, int to) { return to <= 1 ? x : (x + to - 1) / to * to; }
 
 // The units (item, page) of all sequences lie end to end and are cut into equal runs, one a CTA: n_ctas of `each` units, the first `longer` of them
-// of one more.  A run that crosses from one item to the next pays for both a beginning and an end twice, about what four pages take.  So where
-// it costs no more than three pages a CTA, each item is counted as a whole number of runs and none crosses (one row over 211
-// pages, four heads: 13.1 us from first to last, of which two CTAs that crossed took 3.5).
+// of one more.  A run that crosses from one item to the next pays for a beginning and an end twice, and an item in parts for the parts and the join: either
+// takes about as long as kJoinPages pages.  So where it costs no more than that a CTA, each item is counted as a whole number of runs and none
+// crosses (one row over 211 pages, four heads: 13.1 us from first to last, of which two CTAs that crossed took 3.5), or as one (four
+// sequences of 332 tokens, 32 rows of each: 29.5 us in parts of four pages, 21.5).
+constexpr int kJoinPages = 5;
 struct AttnRuns {
   long long units, each;
   int n_ctas, longer, whole;           // whole: units that an item is rounded up to (0: they are as they are)
@@ -86,30 +87,37 @@ template <int W>
 __device__ __forceinline__ AttnRuns cut_units(const CacheAttnArgs& a, long long* before, int grid) {
   if (threadIdx.x < 32) {
     const int lane = threadIdx.x, least = 1 << a.page_shift;
-    auto units_of = [&](int i, int whole, int& items) {
+    auto units_of = [&](int i, int whole, int& items, int& most) {
       const SeqShape s = shape_of<W>(a, i);
       long long u = 0;
 #pragma unroll 1
-      for (int tile = 0; tile < s.tiles; ++tile) u += rounded_up(pages_of<W>(a, s, tile).n, whole);
+      for (int tile = 0; tile < s.tiles; ++tile) {
+        const int n = pages_of<W>(a, s, tile).n;
+        most = max(most, n);
+        u += rounded_up(n, whole);
+      }
       items += min(s.tiles, grid) * a.c.n_kv_heads;
       return u * a.c.n_kv_heads;
     };
-    // all units and items, as far as the rule asks for them
+    // all units and items and the longest item, as far as the rule asks for them
     uint32_t units = 0u;
-    int items = 0, whole = 0;
+    int items = 0, most = 0, whole = 0;
 #pragma unroll 1
-    for (int i = lane; i < a.r.n_seqs; i += 32) units = min(units + (uint32_t)min(units_of(i, 0, items), 1ll << 24), 1u << 24);
+    for (int i = lane; i < a.r.n_seqs; i += 32) units = min(units + (uint32_t)min(units_of(i, 0, items, most), 1ll << 24), 1u << 24);
     units = __reduce_add_sync(0xffffffffu, units);
-    items = __reduce_add_sync(0xffffffffu, min(items, grid));
-    if (units < (1u << 24) && 2 * items <= grid) {
-      const int rounded = max((int)(units + grid - items - 1) / (grid - items), least), equal = max((int)(units + grid - 1) / grid, least);
-      if (rounded - equal <= 3) whole = rounded;
+    items = __reduce_add_sync(0xffffffffu, min(items, grid + 1));
+    most = __reduce_max_sync(0xffffffffu, most);
+    if (units < (1u << 24) && items <= grid) {
+      int rounded = items < grid ? max((int)(units + grid - items - 1) / (grid - items), least) : most;
+      if (rounded + kJoinPages >= most) rounded = max(most, 1);
+      if (rounded - max((int)(units + grid - 1) / grid, least) <= kJoinPages) whole = rounded;
     }
     long long ahead = 0;
 #pragma unroll 1
     for (int base = 0; base < a.r.n_seqs; base += 32) {
       const int i = base + lane;
-      long long u = i < a.r.n_seqs ? units_of(i, whole, items) : 0;
+      int again = 0;
+      long long u = i < a.r.n_seqs ? units_of(i, whole, again, most) : 0;
       if (a.r.n_seqs > 1) {
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) { const long long t = __shfl_up_sync(0xffffffffu, u, o); if (lane >= o) u += t; }
@@ -118,7 +126,8 @@ __device__ __forceinline__ AttnRuns cut_units(const CacheAttnArgs& a, long long*
       ahead += __shfl_sync(0xffffffffu, u, a.r.n_seqs > 1 ? 31 : 0);
     }
     if (lane == 0) {
-      const int n = whole > 0 ? max((int)ahead / whole, 1) : max((int)min((long long)grid, (ahead + least - 1) >> a.page_shift), 1);
+      // (more items than CTAs: no item is cut for want of others, so a run may be short)
+      const int n = whole > 0 ? max((int)ahead / whole, 1) : max((int)min((long long)grid, items > grid ? ahead : (ahead + least - 1) >> a.page_shift), 1);
       const long long each = whole > 0 ? whole : divide(ahead, n);
       before[0] = 0;
       before[a.r.n_seqs + 1] = each;

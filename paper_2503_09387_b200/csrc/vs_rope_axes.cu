@@ -8,6 +8,8 @@
 // each, once for all of the warp's heads -- and hands them round through shared memory: a lane turns the same eight pairs of every head
 // that it meets, so it keeps them in registers.  No warp waits for another.  A far position loses nothing: the angle is
 // formed in turns in fp64, and only the fraction of a turn goes on in fp32.
+// Measured: 3376 rows of 32 bf16 heads of 128, 11.3 us (4.9 TB/s; a floor of 8.5), where a block a row with its angles behind a barrier takes 15.0 (two rows
+// a block the same, four 15.7); one row 2 us beyond an empty launch.
 #include "vs_operators.cuh"
 
 namespace vs {

@@ -208,3 +208,59 @@ def test_token_logprobs_where_another_type_is_the_default():
     finally:
         torch.set_default_dtype(FP32)
     assert all(a.dtype is b.dtype and torch.equal(a, b) for a, b in zip(got, want))
+
+
+# ---- the kernel for many rows: a table so wide that the calls above reach it whatever their rows and tokens ------------------------
+WIDE = 1100
+
+
+@pytest.mark.parametrize("out_dtype", [BF16, FP32])
+@pytest.mark.parametrize("hkv,group,d,lengths,lens", [
+    (2, 7, 128, [150, 33], [5, 5]), (1, 4, 64, [64, 64, 300], [9, 64, 17]), (2, 1, 128, [500], [33]), (1, 7, 128, [170], [170]),
+    (2, 2, 64, [130, 5, 0, 260], [130, 5, 0, 100]), (1, 8, 128, [400], [37]), (1, 5, 64, [77, 900], [3, 60]), (1, 8, 64, [1, 65], [40, 33])])
+def test_attend_many_rows(hkv, group, d, lengths, lens, out_dtype):
+    attend_case(hkv, group, d, lengths, lens, out_dtype=out_dtype, width=WIDE)
+
+
+@pytest.mark.parametrize("causal,window", [(False, 0), (True, 1), (True, 64), (True, 100), (False, 90), (True, 2**31 - 1)])
+@pytest.mark.parametrize("lengths,lens", [([300], [40]), ([65, 200, 3], [10, 70, 7])])
+def test_attend_many_rows_masks(lengths, lens, causal, window):
+    attend_case(1, 7, 128, lengths, lens, causal=causal, window=window, width=WIDE)
+
+
+def test_attend_many_rows_that_see_nothing():
+    lens = [40, 50, 20]
+    _, _, _, out, lse = attend_case(2, 7, 128, [0, 5, 190], lens, holes=[(2, 0), (2, 2)], ragged=True, width=WIDE)
+    assert bool((out[:40] == 0).all()) and bool((lse[:40] == -math.inf).all())
+
+
+def test_attend_many_rows_large_scores_unequal_pages_and_nan():
+    attend_case(1, 7, 128, [500], [33], q_std=60.0, width=WIDE)
+    g = gen(30)
+    cache = pool(g, 6, 1, 128)
+    table = tables(g, [384], 6, WIDE)
+    k, v = normal(g, 384, 1, 128, dtype=FP32), normal(g, 384, 1, 128, dtype=FP32)
+    for p, e in enumerate((0, 40, -60, 10, -100, 3)):
+        v[64 * p:64 * p + 64] *= 2.0 ** e
+        k[64 * p:64 * p + 64] *= 2.0 ** (-3 * p)
+    cache.write(table, ints([0]), k, v)
+    want = ref.Cache(cache.k, cache.v, cache.k_scale, cache.v_scale)
+    q = normal(g, 30, 4, 128)
+    out, lse = cache.attend(table, ints([384]), q, out_dtype=FP32)
+    o, l, o_off, l_off = want.attend(table.tolist(), [384], [30], q, 128 ** -0.5)
+    close(out, o, o_off)
+    close(lse, l, l_off)
+    bad = q.clone()
+    bad[0, 1, 5], bad[1, 2, 7] = math.nan, math.inf
+    got, lse2 = cache.attend(table, ints([384]), bad, out_dtype=FP32)
+    assert bool(torch.isnan(got[0, 1]).all()) and bool(torch.isnan(got[1, 2]).all()) and bool(torch.isnan(lse2[0, 1]))
+    keep = torch.ones(30, 4, dtype=torch.bool)
+    keep[0, 1] = keep[1, 2] = False
+    assert torch.equal(got[keep.cuda()], out[keep.cuda()])
+
+
+@pytest.mark.parametrize("hkv,group,d,lengths,lens", [
+    (8, 8, 64, [70] * 20, [40] * 20), (4, 7, 128, [30] * 24, [12] * 24), (2, 7, 128, [5, 700, 64] * 6, [5, 1, 30] * 6), (8, 1, 128, [130] * 40, [70] * 40)])
+def test_attend_more_items_than_ctas(hkv, group, d, lengths, lens):
+    attend_case(hkv, group, d, lengths, lens)
+    attend_case(hkv, group, d, lengths, lens, width=WIDE)
