@@ -607,6 +607,7 @@ extern "C" int vs_cache_attention(const vs_cache* cache, const vs_cache_queries*
   a.Hq = x->n_q_heads; a.G = G; a.causal = x->causal != 0; a.window = x->window; a.out_fp32 = x->out_dtype;
   a.rcp_g = G == 1 ? 0u : (uint32_t)(((1ull << 32) + G - 1) / G);
   const bool uniform = rows->row_offsets == nullptr;
+  while (a.side_shift < 5 && rows->n_seqs << (a.side_shift + 1) <= 32) ++a.side_shift;
   a.rows_each = uniform ? rows->n_rows / rows->n_seqs : -1;
   a.max_held = rows->table_width >= (1 << 25) ? 0x7fffffff : rows->table_width * kPage;
   // Which sequences have few rows the device knows; the host, from the number of rows, that all of them have (or none, where they have the

@@ -24,6 +24,7 @@ struct CacheAttnArgs {
   int rows_each;                  // of every sequence; -1: by row_offsets
   int max_held;                   // tokens that a sequence's row of the table has pages for
   int page_shift;                 // log2 of the pages that are worth a CTA of their own
+  int side_shift;                 // log2 of the lanes that count a sequence's units: 32 / n_seqs, rounded down to a power of two
   int few_cols, take_few;         // packed rows of a sequence of few rows, at most; whether the launch takes these or the others
 };
 
@@ -62,13 +63,17 @@ __device__ __forceinline__ PageRange pages_of(const CacheAttnArgs& a, const SeqS
 }
 
 __device__ __forceinline__ long long divide(long long x, long long y) { return ((x | y) >> 31) == 0 ? (long long)((uint32_t)x / (uint32_t)y) : x / y; }
-__device__ __forceinline__ int rounded_up(int x, int to) { return to <= 1 ? x : (x + to - 1) / to * to; }
+// x / y, rounded up, 0 <= x <= 2^20: the quotient's relative error of 2^-22 is below 1 / x, so that its whole part is off, if at all, by 1 downwards where y
+// divides x.  (A division of integers is some forty instructions.)
+__device__ __forceinline__ int divide_up(int x, int y) { const int q = (int)__fdividef((float)x, (float)y); return q * y < x ? q + 1 : q; }
+constexpr uint32_t kMostWhole = 1u << 20;
+__device__ __forceinline__ int rounded_up(int x, int to) { return to <= 1 ? x : divide_up(x, to) * to; }
 
 // The units (item, page) of all sequences lie end to end and are cut into equal runs, one a CTA: n_ctas of `each` units, the first `longer` of them
 // of one more.  A run that crosses from one item to the next pays for a beginning and an end twice, and an item in parts for the parts and the join: either
 // takes about as long as kJoinPages pages.  So where it costs no more than that a CTA, each item is counted as a whole number of runs and none
 // crosses (one row over 211 pages, four heads: 13.1 us from first to last, of which two CTAs that crossed took 3.5), or as one (four
-// sequences of 332 tokens, 32 rows of each: 29.5 us in parts of four pages, 21.5).
+// sequences of 332 tokens, 32 rows of each: 29.5 us in parts of four pages, 21.5); with more items than CTAs a run may be several whole ones.
 constexpr int kJoinPages = 5;
 struct AttnRuns {
   long long units, each;
@@ -87,48 +92,59 @@ template <int W>
 __device__ __forceinline__ AttnRuns cut_units(const CacheAttnArgs& a, long long* before, int grid) {
   if (threadIdx.x < 32) {
     const int lane = threadIdx.x, least = 1 << a.page_shift;
+    const int shift = a.side_shift, sub = lane & ((1 << shift) - 1), abreast = 32 >> shift;       // a sequence's tiles are dealt to 2^shift lanes
     auto units_of = [&](int i, int whole, int& items, int& most) {
       const SeqShape s = shape_of<W>(a, i);
       long long u = 0;
 #pragma unroll 1
-      for (int tile = 0; tile < s.tiles; ++tile) {
+      for (int tile = sub; tile < s.tiles; tile += 1 << shift) {
         const int n = pages_of<W>(a, s, tile).n;
         most = max(most, n);
         u += rounded_up(n, whole);
       }
-      items += min(s.tiles, grid) * a.c.n_kv_heads;
+      if (sub == 0) items += min(s.tiles, grid) * a.c.n_kv_heads;
       return u * a.c.n_kv_heads;
     };
     // all units and items and the longest item, as far as the rule asks for them
     uint32_t units = 0u;
     int items = 0, most = 0, whole = 0;
 #pragma unroll 1
-    for (int i = lane; i < a.r.n_seqs; i += 32) units = min(units + (uint32_t)min(units_of(i, 0, items, most), 1ll << 24), 1u << 24);
+    for (int i = lane >> shift; i < a.r.n_seqs; i += abreast) units = min(units + (uint32_t)min(units_of(i, 0, items, most), (long long)kMostWhole), kMostWhole);
     units = __reduce_add_sync(0xffffffffu, units);
-    items = __reduce_add_sync(0xffffffffu, min(items, grid + 1));
-    most = __reduce_max_sync(0xffffffffu, most);
-    if (units < (1u << 24) && items <= grid) {
-      int rounded = items < grid ? max((int)(units + grid - items - 1) / (grid - items), least) : most;
-      if (rounded + kJoinPages >= most) rounded = max(most, 1);
-      if (rounded - max((int)(units + grid - 1) / grid, least) <= kJoinPages) whole = rounded;
+    items = max(__reduce_add_sync(0xffffffffu, min(items, 1 << 20)), 1);
+    most = max(__reduce_max_sync(0xffffffffu, most), 1);
+    int per_cta = 1;                                        // (of runs of `whole` units)
+    if (units < kMostWhole) {
+      const int equal = divide_up((int)units, grid);
+      if (items <= grid) {
+        int runs = (int)__fdividef((float)grid, (float)items);                    // of an item, as many as all of them can have
+        if (runs * items > grid) --runs;
+        int rounded = divide_up(most, max(runs, 1));
+        if (items < grid) rounded = min(rounded, divide_up((int)units, grid - items));
+        rounded = max(rounded, least);
+        if (rounded + kJoinPages >= most) rounded = most;
+        if (rounded - max(equal, least) <= kJoinPages) whole = rounded;
+      } else {
+        per_cta = divide_up(items, grid);
+        if (per_cta * most <= equal + 2 * kJoinPages) whole = most;
+      }
     }
     long long ahead = 0;
 #pragma unroll 1
-    for (int base = 0; base < a.r.n_seqs; base += 32) {
-      const int i = base + lane;
+    for (int base = 0; base < a.r.n_seqs; base += abreast) {
+      const int i = base + (lane >> shift);
       int again = 0;
       long long u = i < a.r.n_seqs ? units_of(i, whole, again, most) : 0;
-      if (a.r.n_seqs > 1) {
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) { const long long t = __shfl_up_sync(0xffffffffu, u, o); if (lane >= o) u += t; }
-      }
-      if (i < a.r.n_seqs) before[i + 1] = ahead + u;
-      ahead += __shfl_sync(0xffffffffu, u, a.r.n_seqs > 1 ? 31 : 0);
+      for (int o = 1; o < 32; o <<= 1) { const long long t = __shfl_up_sync(0xffffffffu, u, o); if (lane >= o) u += t; }
+      if (i < a.r.n_seqs && sub + 1 == 1 << shift) before[i + 1] = ahead + u;
+      ahead += __shfl_sync(0xffffffffu, u, 31);
     }
     if (lane == 0) {
       // (more items than CTAs: no item is cut for want of others, so a run may be short)
-      const int n = whole > 0 ? max((int)ahead / whole, 1) : max((int)min((long long)grid, items > grid ? ahead : (ahead + least - 1) >> a.page_shift), 1);
-      const long long each = whole > 0 ? whole : divide(ahead, n);
+      const int run = whole * per_cta;
+      const int n = whole > 0 ? max(divide_up((int)ahead, run), 1) : max((int)min((long long)grid, items > grid ? ahead : (ahead + least - 1) >> a.page_shift), 1);
+      const long long each = whole > 0 ? run : divide(ahead, n);
       before[0] = 0;
       before[a.r.n_seqs + 1] = each;
       before[a.r.n_seqs + 2] = n | (whole > 0 ? 0 : (ahead - each * n) << 32);
