@@ -72,7 +72,6 @@ __global__ void __launch_bounds__(kThreads) cache_attention_few_kernel(const __g
   extern __shared__ __align__(128) uint8_t smem[];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, q4 = lane & 3;
   long long* before = reinterpret_cast<long long*>(smem + F::kBefore);
-  pdl_launch_dependents();
   const AttnRuns runs = cut_units<W>(a, before, (int)gridDim.x);
   const int cta = (int)blockIdx.x;
   if (tid == 0) a.joins[cta] = make_int4(0, 0, 0, 0);
@@ -520,7 +519,8 @@ __global__ void __launch_bounds__(kJoinThreads, kJoinBlocks / 148) cache_attenti
   if constexpr (kMany) join_items<kManyWide, D>(a, many.joins, many.parts, many.ctas, sm);
 }
 
-// as many as are resident: three an SM of 168 registers a thread, two of 255
+// as many as are resident: three an SM of 168 registers a thread, two of 255 (sixteen sequences of 13440 tokens, two rows of seven heads: 58.7 us; in one and a half
+// rounds 78.2)
 int few_ctas(int cols) { return cols <= 8 ? kFewCtas : 2 * 148; }
 template <int D, int NT>
 int launch_few(const CacheAttnArgs& a, cudaStream_t st) {
@@ -537,6 +537,7 @@ int launch_join(const CacheAttnArgs& a, Parts few, Parts many, cudaStream_t st) 
   cfg.gridDim = dim3(kJoinBlocks);
   cfg.blockDim = dim3(kJoinThreads);
   cfg.stream = st;
+  // (Its blocks come when those ahead have ended; let in from the start, they take 1.5 us from a call of 13.8 that they wait through.)
   cudaLaunchAttribute at = {};
   at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
   at.val.programmaticStreamSerializationAllowed = 1;
@@ -613,8 +614,8 @@ extern "C" int vs_cache_attention(const vs_cache* cache, const vs_cache_queries*
   // Which sequences have few rows the device knows; the host, from the number of rows, that all of them have (or none, where they have the
   // same number each).  Either kind has its kernel; what their CTAs left in parts one launch joins.
   const long long most = (long long)(uniform ? a.rows_each : rows->n_rows) * G;
-  // The kernel of few rows takes a sequence of up to 32 packed rows, two of its tiles (seven heads a group, four KV heads, three rows: 17.1 us against the
-  // other's 20.6 over 13440 tokens, 97 against 106 for sixteen sequences; six rows, three tiles: 20.7 and 20.6, 136 and 108), and any while there are few
+  // The kernel of few rows takes a sequence of up to 32 packed rows, two of its tiles (seven heads a group, four KV heads, four rows: 16.0 us against the
+  // other's 19.2 over 13440 tokens, 97 against 107 for sixteen sequences; six rows, three tiles: 20.7 and 20.6, 136 and 108), and any while there are few
   // tiles and pages: the other one's items begin and end slowly (32 rows over 300 tokens 16.7 and 20.8, over 1500 22.3 and 23.7, over 6000 37.6 and 25.2).
   const long long tiles = uniform ? (long long)rows->n_seqs * ((a.rows_each * G + kFewWide - 1) / kFewWide) : (long long)rows->n_rows * G / kFewWide + rows->n_seqs;
   const long long items = tiles * cache->n_kv_heads;

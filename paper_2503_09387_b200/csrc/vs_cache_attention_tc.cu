@@ -128,7 +128,6 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attention_tc_kernel(const _
   volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + L::kSlotWord + 4);
   long long* before = reinterpret_cast<long long*>(smem + L::kBefore);
 
-  pdl_launch_dependents();
   if (warp == kIssuerWarp) {
     for (uint32_t x = (uint32_t)lane; x < (uint32_t)L::kBars; x += 32u)
       mbar_init(ctl + 8u * x, (x >= kRing && x < 3 * kRing) || (x >= kTileBars && x < kTileBars + 3 * kTiles) ? 4u : (x >= 3 * kRing && x < 4 * kRing ? 2u : 1u));       // (converters, softmax: four warps; issuers: two)
