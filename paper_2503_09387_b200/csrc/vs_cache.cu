@@ -9,7 +9,7 @@
 // What bounds them: the rows' bytes and the codes'.  A block takes the rows of one page and head, keys or values: it holds them in
 // registers from the load to the codes, the maximum in between, so that they are read once.  Blocks find their page by
 // the sequences' rows on the device; the host knows how many there can be.
-// Measured: 13440 tokens of four heads of 128 read as bf16 (13.8 MB in, 27.5 MB out) 9.6 us, 4.3 TB/s; 2571 written as bf16 8 us, one of each of sixteen
+// Measured: 13440 tokens of four heads of 128 read as bf16 (13.8 MB in, 27.5 MB out) 9.6 us, 4.3 TB/s; 2950 written from bf16 8 us, one of each of sixteen
 // sequences 3: beyond the launch, two dependent loads (the sequence's length, its page) and the rows.
 #include "vs_operators.cuh"
 
