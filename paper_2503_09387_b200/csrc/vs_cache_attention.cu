@@ -610,7 +610,7 @@ extern "C" int vs_cache_attention(const vs_cache* cache, const vs_cache_queries*
   const bool uniform = rows->row_offsets == nullptr;
   while (a.side_shift < 5 && rows->n_seqs << (a.side_shift + 1) <= 32) ++a.side_shift;
   a.rows_each = uniform ? rows->n_rows / rows->n_seqs : -1;
-  a.max_held = rows->table_width >= (1 << 25) ? 0x7fffffff : rows->table_width * kPage;
+  a.max_held = rows->table_width >= (1 << 25) ? 0x7fffffff - (kPage - 1) : rows->table_width * kPage;      // (whole pages)
   // Which sequences have few rows the device knows; the host, from the number of rows, that all of them have (or none, where they have the
   // same number each).  Either kind has its kernel; what their CTAs left in parts one launch joins.
   const long long most = (long long)(uniform ? a.rows_each : rows->n_rows) * G;
