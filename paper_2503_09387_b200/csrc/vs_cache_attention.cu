@@ -616,10 +616,11 @@ extern "C" int vs_cache_attention(const vs_cache* cache, const vs_cache_queries*
   const long long most = (long long)(uniform ? a.rows_each : rows->n_rows) * G;
   // The kernel of few rows takes a sequence of up to 32 packed rows, two of its tiles (seven heads a group, four KV heads, four rows: 16.0 us against the
   // other's 19.2 over 13440 tokens, 97 against 107 for sixteen sequences; six rows, three tiles: 20.7 and 20.6, 136 and 108), and any while there are few
-  // tiles and pages: the other one's items begin and end slowly (32 rows over 300 tokens 16.7 and 20.8, over 1500 22.3 and 23.7, over 6000 37.6 and 25.2).
+  // tiles and pages: the other one's items begin and end slowly (32 rows over 300 tokens 14.1 and 21.0, over 1500 19.5 and 23.3, over 6000 31.4 and 24.7; four
+  // sequences of 32 rows over 300 tokens, 1568 tiles times pages of a table, 16.5 and 21.5; of 12 over 1500, 2496, 22.4 and 18.5).
   const long long tiles = uniform ? (long long)rows->n_seqs * ((a.rows_each * G + kFewWide - 1) / kFewWide) : (long long)rows->n_rows * G / kFewWide + rows->n_seqs;
   const long long items = tiles * cache->n_kv_heads;
-  a.few_cols = items <= few_ctas(kFewWide) && items * rows->table_width <= 1024 ? 0x7fffffff : 32;
+  a.few_cols = items <= few_ctas(kFewWide) && items * rows->table_width <= 1600 ? 0x7fffffff : 32;
   const bool any_few = most <= a.few_cols || !uniform, any_many = most > a.few_cols;
   const int cols = any_few ? (most <= 8 ? 8 : kFewWide) : 0;
   const Parts few = {reinterpret_cast<int4*>(ws + kFewJoinsAt), reinterpret_cast<float*>(ws + kPartsAt), few_ctas(cols)};
