@@ -409,8 +409,8 @@ int vs_cache_attention(const vs_cache* cache, const vs_cache_queries* queries, v
  *   logprob[r] = x_t - log sum_j e^{x_j}, t = tokens[r];  entropy[r] = -sum_j p_j log p_j (nats);
  *   rank[r] = how many tokens come before t in the order "larger logit, else lower index, NaN below every
  *   number" (0: t is vs_lm_head's next_token);  top_index, top_logprob [rows][top]: the first `top` of that order.
- * logits: DEVICE [rows][vocab] of dtype, row_stride between rows, aligned to their type (faster when rows
- *   begin on 16-byte boundaries); -inf is a token that cannot be.
+ * logits: DEVICE [rows][vocab] of dtype, row_stride between rows, aligned to their type; -inf is a token
+ *   that cannot be.
  * tokens: DEVICE int32 [rows], NULL only without logprob and rank; a negative one asks nothing (logprob 0, rank -1), one >= vocab gets NaN and -1.
  * Outputs: DEVICE, each may be NULL (top_index not when top > 0); all fp32 but rank and top_index (int32).
  * A row that holds NaN or +inf has NaN for what is summed; one of -inf only has -inf and entropy 0.

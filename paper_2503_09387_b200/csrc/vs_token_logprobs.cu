@@ -77,41 +77,23 @@ __device__ __forceinline__ unsigned long long key_of(uint32_t o, int i) { return
 template <typename T>
 struct Vec { static constexpr int n = 16 / (int)sizeof(T); };
 
-// the logits of vector i of a row, all of which are there
-template <typename T, bool kVector>
-__device__ __forceinline__ uint4 fetch_whole(const T* row, int i) {
+// A row is read in vectors of 16 bytes from the last boundary at or ahead of its first logit, which is then number `off`; [off, end) are its logits' numbers.
+// Vector i: what lies outside the row as -inf, and not read.
+template <typename T>
+__device__ __forceinline__ uint4 fetch(const T* row, int i, int off, int end) {
   constexpr int V = Vec<T>::n;
-  if constexpr (kVector) {
-    return __ldg(reinterpret_cast<const uint4*>(row) + i);
-  } else {
-    uint32_t w[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      if constexpr (sizeof(T) == 4) {
-        w[j] = __float_as_uint(row[i * V + j]);
-      } else {
-        const uint16_t* r = reinterpret_cast<const uint16_t*>(row) + i * V + 2 * j;
-        w[j] = (uint32_t)r[0] | ((uint32_t)r[1] << 16);
-      }
-    }
-    return make_uint4(w[0], w[1], w[2], w[3]);
-  }
-}
-// those of any vector: -inf behind the end of the row
-template <typename T, bool kVector>
-__device__ __forceinline__ uint4 fetch(const T* row, int i, int vocab) {
-  constexpr int V = Vec<T>::n;
-  if (kVector && (i + 1) * V <= vocab) return __ldg(reinterpret_cast<const uint4*>(row) + i);
+  if (i * V >= off && (i + 1) * V <= end) return __ldg(reinterpret_cast<const uint4*>(row) + i);
   const uint32_t nothing = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;
-  if (i * V >= vocab) return make_uint4(nothing, nothing, nothing, nothing);
+  if (i * V >= end) return make_uint4(nothing, nothing, nothing, nothing);
   uint32_t w[4];
+  auto there = [&](int at) { return at >= off && at < end; };
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     if constexpr (sizeof(T) == 4) {
-      w[j] = i * V + j < vocab ? __float_as_uint(row[i * V + j]) : 0xff800000u;
+      w[j] = there(i * V + j) ? __float_as_uint(row[i * V + j]) : 0xff800000u;
     } else {
       const uint16_t* r = reinterpret_cast<const uint16_t*>(row);
-      const uint32_t lo = i * V + 2 * j < vocab ? r[i * V + 2 * j] : 0xff80u, hi = i * V + 2 * j + 1 < vocab ? r[i * V + 2 * j + 1] : 0xff80u;
+      const uint32_t lo = there(i * V + 2 * j) ? r[i * V + 2 * j] : 0xff80u, hi = there(i * V + 2 * j + 1) ? r[i * V + 2 * j + 1] : 0xff80u;
       w[j] = lo | (hi << 16);
     }
   }
@@ -150,43 +132,47 @@ __device__ __forceinline__ float max_nan(float a, float b) {
   return m;
 }
 
-template <typename T, bool kVector>
+// kOff: rows that begin off a boundary of 16 bytes (197 rows of 152064 on them, as if they might not: 34.8 us against 32.4)
+template <typename T, bool kOff>
 __global__ void __launch_bounds__(kThreads, 2) token_logprobs_kernel(const __grid_constant__ ScoreArgs a) {
   __shared__ Shared sm;
   constexpr int V = Vec<T>::n, E = 16, U = E / V;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int C = a.cluster, row_i = (int)blockIdx.x / C, rank = (int)blockIdx.x - row_i * C;
   const T* row = static_cast<const T*>(a.logits) + (long long)row_i * a.row_stride;
-  const int nv = (a.vocab + V - 1) / V;
+  const int off = kOff ? (int)((reinterpret_cast<uintptr_t>(row) & 15u) / sizeof(T)) : 0, end = off + a.vocab;
+  row -= off;
+  const int nv = (end + V - 1) / V;
   const int v0 = (int)((long long)nv * rank / C), v1 = (int)((long long)nv * (rank + 1) / C);
-  const int whole_v = min(v1, a.vocab / V), steps = (v1 - v0 + U * kThreads - 1) / (U * kThreads);
+  const int whole_v = min(v1, end / V), steps = (v1 - v0 + U * kThreads - 1) / (U * kThreads);
   // the vectors of one step: without a question where all threads have all of theirs
   uint4 next[U];
-  auto load = [&](int v) {
-    if (v - tid + U * kThreads <= whole_v) {
+  auto load = [&](int v, bool whole) {
+    if (whole && v - tid + U * kThreads <= whole_v) {
 #pragma unroll
-      for (int j = 0; j < U; ++j) next[j] = fetch_whole<T, kVector>(row, v + j * kThreads);
+      for (int j = 0; j < U; ++j) next[j] = __ldg(reinterpret_cast<const uint4*>(row) + (v + j * kThreads));
     } else {
 #pragma unroll
-      for (int j = 0; j < U; ++j) next[j] = fetch<T, kVector>(row, v + j * kThreads, v + j * kThreads < v1 ? a.vocab : 0);
+      for (int j = 0; j < U; ++j) next[j] = fetch(row, v + j * kThreads, off, v + j * kThreads < v1 ? end : 0);
     }
   };
-  load(v0 + tid);
+  load(v0 + tid, off == 0 || v0 > 0);
   const int token = a.tokens != nullptr ? a.tokens[row_i] : -1;
   const bool has_token = token >= 0 && token < a.vocab;
+  const int token_at = token + off;
   const float nan = __int_as_float(0x7fc00000);
   float xt = nan;                      // (no token: nothing comes before it)
   if (has_token) {
-    if constexpr (sizeof(T) == 4) xt = row[token];
-    else xt = __bfloat162float(row[token]);
+    if constexpr (sizeof(T) == 4) xt = row[token_at];
+    else xt = __bfloat162float(row[token_at]);
   }
   const bool xt_nan = has_token && xt != xt;
   // what reaches this comes before the token: its logit in the vectors ahead of the token's, the next larger one from there on
   const float behind = next_up(xt);
-  const int token_v = has_token ? token / V : 0, ahead = min(token_v, v1);
+  const int token_v = has_token ? token_at / V : 0, ahead = min(token_v, v1);
 
   // ---- one pass: largest, sums of the others, place of the token -----------------------------------------------
-  float best_x = -INFINITY, ref = 0.f, ref2 = 0.f, off = 0.f, sum = 0.f, sum_u = 0.f;  // ref2 = ref log2e - off, as it is rounded
+  float best_x = -INFINITY, ref = 0.f, ref2 = 0.f, slip = 0.f, sum = 0.f, sum_u = 0.f;  // ref2 = ref log2e - slip, as it is rounded
   int n_before = 0;
   auto shift_sums = [&](float by) {    // by so many powers of two
     by = fmaxf(by, -1000.f);
@@ -208,12 +194,12 @@ __global__ void __launch_bounds__(kThreads, 2) token_logprobs_kernel(const __gri
         n_before += x >= reach ? 1 : 0;
       }
     }
-    if (step + 1 < steps) load(v + U * kThreads);
+    if (step + 1 < steps) load(v + U * kThreads, true);
     if (best_x > -INFINITY && (was == -INFINITY || best_x - ref > 40.f)) {
       const bool finite = fabsf(best_x) < kHuge;
-      const float to2 = finite ? best_x * kLog2e : 0.f, to_off = finite ? fmaf(best_x, kLog2e, -to2) : 0.f;
-      if (was != -INFINITY) shift_sums(fmaf(ref - best_x, kLog2e, to_off - off));
-      ref = best_x; ref2 = to2; off = to_off;
+      const float to2 = finite ? best_x * kLog2e : 0.f, to_slip = finite ? fmaf(best_x, kLog2e, -to2) : 0.f;
+      if (was != -INFINITY) shift_sums(fmaf(ref - best_x, kLog2e, to_slip - slip));
+      ref = best_x; ref2 = to2; slip = to_slip;
     }
     float s = 0.f, u = 0.f;
     if (fabsf(ref) < kHuge) {
@@ -238,24 +224,25 @@ __global__ void __launch_bounds__(kThreads, 2) token_logprobs_kernel(const __gri
   if (best_x != best_x) {                                              // NaN among them: the largest number, for the alternatives
     best_x = -INFINITY;
     for (int v = v0 + tid; v < v1; v += kThreads) {
-      const uint4 w = fetch<T, kVector>(row, v, a.vocab);
+      const uint4 w = fetch(row, v, off, end);
 #pragma unroll
       for (int e = 0; e < V; ++e) best_x = fmaxf(best_x, element<T>(w, e));
     }
   }
   if (xt_nan) {                                                        // behind every number, and NaN of a lower index
     for (int v = v0 + tid; v < v1; v += kThreads)
-      for (int i = v * V; i < min((v + 1) * V, a.vocab); ++i) n_before += (float)row[i] == (float)row[i] || i < token ? 1 : 0;
+      for (int i = max(v * V, off); i < min((v + 1) * V, end); ++i) n_before += (float)row[i] == (float)row[i] || i < token_at ? 1 : 0;
   }
   Part p = {best_x, 0.f, 0.f, 0u};
   if (best_x > -INFINITY) {
-    shift_sums(fmaf(ref - best_x, kLog2e, -off));                      // (2^-58 at the least)
+    shift_sums(fmaf(ref - best_x, kLog2e, -slip));                      // (2^-58 at the least)
     p.s = sum;
     p.u = sum_u * kLn2;
   }
   const uint32_t own_max = ordered(p.m);
   if (has_token && token_v >= v0 && token_v < v1 && tid == 0)          // equal ones ahead of the token in its own vector
-    for (int i = token_v * V; i < token; ++i) n_before += (float)row[i] == xt ? 1 : 0;
+    for (int i = max(token_v * V, off); i < token_at; ++i) n_before += (float)row[i] == xt ? 1 : 0;
+  if (v0 == 0 && token_v > 0 && xt == -INFINITY && tid == 0) n_before -= off;            // what is not there counted as equal ones
   p.join_lanes(32);
   n_before = __reduce_add_sync(0xffffffffu, n_before);
   const bool any_odd = __any_sync(0xffffffffu, odd);
@@ -314,7 +301,7 @@ __global__ void __launch_bounds__(kThreads, 2) token_logprobs_kernel(const __gri
         for (int e = 1; e < V; ++e) most = fmaxf(most, element<T>(w, e));
         if (!(most >= reach)) return;
 #pragma unroll 1
-        for (int at = v * V; at < min((v + 1) * V, a.vocab); ++at) {    // (few do)
+        for (int at = max(v * V, off); at < min((v + 1) * V, end); ++at) {      // (few do)
           const uint32_t o = ordered((float)row[at]);
           if (o < bound) continue;
           if (o > bound) { const int to = atomicAdd(&sm.n_above, 1); if (to < kAbove) sm.above[to] = key_of(o, at); }
@@ -328,7 +315,7 @@ __global__ void __launch_bounds__(kThreads, 2) token_logprobs_kernel(const __gri
           for (int v = first + lane * kThreads; v < v1; v += 128 * kThreads) {
             uint4 w[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) w[j] = fetch<T, kVector>(row, v + 32 * j * kThreads, v + 32 * j * kThreads < v1 ? a.vocab : 0);
+            for (int j = 0; j < 4; ++j) w[j] = fetch(row, v + 32 * j * kThreads, off, v + 32 * j * kThreads < v1 ? end : 0);
 #pragma unroll
             for (int j = 0; j < 4; ++j) look(v + 32 * j * kThreads, w[j]);
           }
@@ -337,7 +324,7 @@ __global__ void __launch_bounds__(kThreads, 2) token_logprobs_kernel(const __gri
 #pragma unroll 1
         for (int i = tid; i < n_read; i += kThreads) {
           const int h = i / per, v = v0 + sm.holder[h] + (i - h * per) * kThreads;
-          look(v, fetch<T, kVector>(row, v, v < v1 ? a.vocab : 0));
+          look(v, fetch(row, v, off, v < v1 ? end : 0));
         }
       }
       __syncthreads();
@@ -367,11 +354,11 @@ __global__ void __launch_bounds__(kThreads, 2) token_logprobs_kernel(const __gri
         for (int round = n_found > kEqual ? 0 : 1; round < 3; ++round) {
           const uint32_t wanted = round == 0 ? bound : (round == 1 ? kLeastNumber - 1u : 0u);
           for (int v = v0; v < v1 && have < k - n_above; v += 32) {
-            const uint4 w = fetch<T, kVector>(row, v + lane, v + lane < v1 ? a.vocab : 0);
+            const uint4 w = fetch(row, v + lane, off, v + lane < v1 ? end : 0);
             uint32_t hits = 0u;
 #pragma unroll
             for (int e = 0; e < V; ++e)
-              hits |= (v + lane < v1 && (v + lane) * V + e < a.vocab && ordered(element<T>(w, e)) == wanted) ? 1u << e : 0u;
+              hits |= (v + lane < v1 && (v + lane) * V + e >= off && (v + lane) * V + e < end && ordered(element<T>(w, e)) == wanted) ? 1u << e : 0u;
             int sum = __popc(hits);
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) { const int t = __shfl_up_sync(0xffffffffu, sum, o); if (lane >= o) sum += t; }
@@ -466,12 +453,12 @@ __global__ void __launch_bounds__(kThreads, 2) token_logprobs_kernel(const __gri
   }
   if (tid < k) {
     const unsigned long long key = best[tid];
-    if (a.top_index != nullptr) a.top_index[(long long)row_i * k + tid] = 0x7fffffff - (int)(uint32_t)key;
+    if (a.top_index != nullptr) a.top_index[(long long)row_i * k + tid] = 0x7fffffff - (int)(uint32_t)key - off;
     if (a.top_logprob != nullptr) a.top_logprob[(long long)row_i * k + tid] = logprob_of(of_ordered((uint32_t)(key >> 32)));
   }
 }
 
-template <typename T, bool kVector>
+template <typename T, bool kOff>
 int launch(const ScoreArgs& a, cudaStream_t st) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(a.rows * a.cluster));
@@ -482,7 +469,7 @@ int launch(const ScoreArgs& a, cudaStream_t st) {
   at.val.clusterDim.x = (unsigned)a.cluster; at.val.clusterDim.y = 1; at.val.clusterDim.z = 1;
   cfg.attrs = &at;
   cfg.numAttrs = a.cluster > 1 ? 1 : 0;
-  return cudaLaunchKernelEx(&cfg, token_logprobs_kernel<T, kVector>, a) == cudaSuccess ? launched() : VS_ERR_CUDA;
+  return cudaLaunchKernelEx(&cfg, token_logprobs_kernel<T, kOff>, a) == cudaSuccess ? launched() : VS_ERR_CUDA;
 }
 
 }  // namespace
@@ -511,8 +498,8 @@ extern "C" int vs_token_logprobs(const vs_scores* x, void* cuda_stream) {
   // two: 3.9 TB/s; 256 rows 33.3: 4.7 TB/s).
   const int vectors = (int)((x->vocab + 16 / el - 1) / (16 / el)), most = x->rows <= 8 ? 8 : (x->rows <= 74 ? 4 : 1);
   while (a.cluster < most && vectors >= 8192 * a.cluster) a.cluster *= 2;
-  const bool vector = aligned(x->logits, 16) && (x->row_stride * (int64_t)el) % 16 == 0;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  if (x->dtype == 1) return vector ? launch<float, true>(a, st) : launch<float, false>(a, st);
-  return vector ? launch<bf16, true>(a, st) : launch<bf16, false>(a, st);
+  const bool off = !aligned(x->logits, 16) || (x->rows > 1 && (x->row_stride * (int64_t)el) % 16 != 0);
+  if (x->dtype == 1) return off ? launch<float, true>(a, st) : launch<float, false>(a, st);
+  return off ? launch<bf16, true>(a, st) : launch<bf16, false>(a, st);
 }

@@ -264,3 +264,21 @@ def test_attend_many_rows_large_scores_unequal_pages_and_nan():
 def test_attend_more_items_than_ctas(hkv, group, d, lengths, lens):
     attend_case(hkv, group, d, lengths, lens)
     attend_case(hkv, group, d, lengths, lens, width=WIDE)
+
+
+@pytest.mark.parametrize("dtype", [FP32, BF16])
+@pytest.mark.parametrize("rows,vocab", [(9, 70003), (80, 9001), (3, 140001), (2, 5)])
+def test_token_logprobs_rows_off_the_boundaries(rows, vocab, dtype):
+    """Rows side by side of an odd size, and inside a wider tensor: first vectors in part ahead of the row, -inf among them and as the token's."""
+    g = gen(vocab)
+    for first, width in ((0, vocab), (1, vocab + 3), (3, vocab + 6)):
+        wide = torch.full((rows, width), 1e30, device="cuda")
+        x = normal(g, rows, vocab, std=2.0, dtype=FP32)
+        x[::2, : vocab // 2] = -math.inf
+        x[1::4] = -math.inf
+        wide[:, first:first + vocab] = x
+        tokens = torch.randint(0, vocab, (rows,), device="cuda", generator=g, dtype=torch.int32)
+        tokens[::3] = vocab // 2 - 1
+        tokens[1::3] = min(vocab - 1, 9)
+        for top in (0, min(20, vocab)):
+            check_scores(wide.to(dtype)[:, first:first + vocab], tokens, top)
