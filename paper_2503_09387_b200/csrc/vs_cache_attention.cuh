@@ -102,10 +102,11 @@ __device__ __forceinline__ AttnRuns cut_units(const CacheAttnArgs& a, long long*
         most = max(most, n);
         u += rounded_up(n, whole);
       }
-      if (sub == 0) items += min(s.tiles, grid) * a.c.n_kv_heads;
+      if (sub == 0) items += (int)min((long long)s.tiles * a.c.n_kv_heads, (long long)kMostWhole);
       return u * a.c.n_kv_heads;
     };
-    // all units and items and the longest item, as far as the rule asks for them
+    // all units and items and the longest item, as far as the rule asks for them.  (An item has a unit at least: where the units are fewer than
+    // kMostWhole the items are all counted, and with them the runs below are at most `grid`: no run may be left without a CTA.)
     uint32_t units = 0u;
     int items = 0, most = 0, whole = 0;
 #pragma unroll 1

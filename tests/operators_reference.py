@@ -160,3 +160,47 @@ def token_logprobs(logits, tokens, top):
         got.append((0.0 if t < 0 else (math.nan if t >= len(x) else lp(t)), entropy, order.index(t) if 0 <= t < len(x) else -1,
                     order[:top], [lp(i) for i in order[:top]]))
     return got
+
+
+def attend_at_once(cache, table, lengths, lens, q, scale, causal=True, window=0, chunk=512):
+    """Cache.attend of a PageCache by matrix products in 64 bits where its tensors lie, for calls of many rows.  Every token of a
+    sequence has a page.  -> (out, lse, bound on |error| of the rows before their rounding, bound of lse), with |k| |q| in the
+    place of |k| . |q|, which it is never below."""
+    hkv, d, group = cache.n_kv_heads, cache.head_dim, q.shape[1] // cache.n_kv_heads
+    out, off = (torch.zeros(q.shape, dtype=torch.float64, device=q.device) for _ in range(2))
+    lse = torch.full(q.shape[:2], -math.inf, dtype=torch.float64, device=q.device)
+    lse_off = torch.zeros(q.shape[:2], dtype=torch.float64, device=q.device)
+    first = 0
+    for i, n in enumerate(lens):
+        total = lengths[i]
+        pages = table[i, :(total + PAGE - 1) // PAGE].long()
+        # [Hkv, tokens, D]
+        k, v = ((codes[pages].double() * s[pages].double()[..., None, None]).transpose(0, 1).flatten(1, 2)[:, :total]
+                for codes, s in ((cache.k, cache.k_scale), (cache.v, cache.v_scale)))
+        key = torch.arange(total, device=q.device)
+        for r in range(0, n, chunk):
+            m = min(chunk, n - r)
+            pos = (total - n + torch.arange(r, r + m, device=q.device)).repeat(group)[:, None]
+            seen = (key <= pos) if causal else torch.ones((m * group, total), dtype=torch.bool, device=q.device)
+            if window:
+                seen = seen & (key > pos - window)
+            some = seen.any(-1)
+            for h in range(hkv):
+                rows, heads = slice(first + r, first + r + m), slice(h * group, (h + 1) * group)
+                x = q[rows, heads].double().transpose(0, 1).flatten(0, 1)                    # [group rows, D]
+                s = (x @ k[h].T * scale).masked_fill(~seen, -math.inf)
+                p = torch.softmax(s, -1).nan_to_num(0.0)
+                hidden = ~seen.any(0)                                                        # (may hold anything)
+                vh = v[h].masked_fill(hidden[:, None], 0.0)
+                size = k[h].masked_fill(hidden[:, None], 0.0).norm(dim=-1).max() * x.norm(dim=-1) * scale if total else torch.zeros_like(x[:, 0])
+                ds = (d + 4) * 2.0 ** -24 * size + 6 * 2.0 ** -24 * (size + 256)
+                dw = 2 * ds + 2.0 ** -11 + (seen.sum(-1) + 64) * 2.0 ** -24
+                far = 2.0 ** -38 * vh.abs().amax(0) * seen.sum(-1)[:, None] if total else 0.0
+                back = lambda t: t.unflatten(0, (group, m)).transpose(0, 1)
+                out[rows, heads] = back(p @ vh)
+                off[rows, heads] = back(2 * dw[:, None] * (p @ vh.abs()) + far)
+                l = torch.logsumexp(s, -1)
+                lse[rows, heads] = back(l)
+                lse_off[rows, heads] = back(torch.where(some, dw - 2.0 ** -11 + 2.0 ** -22 * l.abs(), 0.0))
+        first += n
+    return out, lse, off, lse_off
