@@ -44,7 +44,8 @@ struct Tc {
   static constexpr int kBars = 4 * kRing + 7 * kTiles;
   static constexpr int kFlags = kCtl + 8 * kBars;       // [place] first and end of the rows of the raw tile that count (end 0: the page is not there)
   static constexpr int kSlotWord = kFlags + 8 * kRing;
-  static constexpr int kBefore = (kSlotWord + 8 + 7) / 8 * 8;
+  static constexpr int kPlaces = (kSlotWord + 8 + 15) / 16 * 16;               // [warp] where its last item lies
+  static constexpr int kBefore = kPlaces + 16 * (kThreads / 32);
   static int bytes(int n_seqs) { return kBefore + 8 * (n_seqs + 1 + kCutWords); }
 };
 
@@ -127,7 +128,9 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attention_tc_kernel(const _
   volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(smem + L::kSlotWord);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + L::kSlotWord + 4);
   long long* before = reinterpret_cast<long long*>(smem + L::kBefore);
+  ItemPlace* const place_of = reinterpret_cast<ItemPlace*>(smem + L::kPlaces) + warp;
 
+  if (lane == 0) *place_of = {0, -1, 0};
   if (warp == kIssuerWarp) {
     for (uint32_t x = (uint32_t)lane; x < (uint32_t)L::kBars; x += 32u)
       mbar_init(ctl + 8u * x, (x >= kRing && x < 3 * kRing) || (x >= kTileBars && x < kTileBars + 3 * kTiles) ? 4u : (x >= 3 * kRing && x < 4 * kRing ? 2u : 1u));       // (converters, softmax: four warps; issuers: two)
@@ -154,7 +157,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attention_tc_kernel(const _
       uint32_t done = 0;                                                   // tiles of the items so far
       bool ok = true;
       for (long long u = u_begin; u < u_end && ok;) {
-        const AttnItem it = item_at<kWide>(a, before, runs, u, u_end);
+        const AttnItem it = item_at<kWide>(a, before, runs, u, u_end, place_of);
         if (it.n < 1) break;
         u += it.span;
         // keys that any row of the item sees
@@ -206,7 +209,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attention_tc_kernel(const _
       uint32_t done = 0, g = 0, n_items = 0;                               // page tiles of the items so far; pages and items of the row tile
       bool ok = true;
       for (long long u = u_begin; u < u_end && ok;) {
-        const AttnItem it = item_at<kWide>(a, before, runs, u, u_end);
+        const AttnItem it = item_at<kWide>(a, before, runs, u, u_end, place_of);
         if (it.n < 1) break;
         u += it.span;
         const bool mine = it.n_cols > i * kRows;                           // (else the page tiles are only let go)
@@ -276,7 +279,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attention_tc_kernel(const _
     uint32_t end = 0, x = half;                                            // page tiles to the end of the item; the tile at hand
     bool ok = true;
     for (long long u = u_begin; u < u_end && ok;) {
-      const AttnItem it = item_at<kWide>(a, before, runs, u, u_end);
+      const AttnItem it = item_at<kWide>(a, before, runs, u, u_end, place_of);
       if (it.n < 1) break;
       u += it.span;
       end += 2u * (uint32_t)it.n;
@@ -326,7 +329,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attention_tc_kernel(const _
     uint32_t g = 0;                                                        // pages so far
     bool ok = true;
     for (long long u = u_begin; u < u_end && ok;) {
-      const AttnItem it = item_at<kWide>(a, before, runs, u, u_end);
+      const AttnItem it = item_at<kWide>(a, before, runs, u, u_end, place_of);
       if (it.n < 1) break;
       u += it.span;
       const int col = i * kRows + row;                                     // packed row of the item

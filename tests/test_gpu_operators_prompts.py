@@ -52,3 +52,24 @@ def test_attend_a_prompt_is_its_chunks():
         o, l = cache.attend(table, ints([end]), q[r:end], out_dtype=FP32)
         assert bool(((o - out[r:end]).abs() <= 2 * o_off[r:end] + 2.0 ** -22 * out[r:end].abs()).all())
         assert bool(((l - lse[r:end]).abs() <= 2 * l_off[r:end]).all())
+
+
+def test_attend_time_of_many_rows_over_few_keys():
+    """Four times the rows over 64 keys take about four times as long, not sixteen times: an item is not looked for from the first tile."""
+    cache = binding.PageCache.empty(1, 4, 64)
+    cache.write(ints([[0]]), ints([0]), normal(gen(1), 64, 4, 64), normal(gen(2), 64, 4, 64))
+
+    def time_of(n):
+        q = normal(gen(3), n, 32, 64)
+        out, lse = torch.empty_like(q), torch.empty((n, 32), device="cuda")
+        best = []
+        for _ in range(4):
+            a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            a.record()
+            cache.attend(ints([[0]]), ints([64]), q, out=out, lse=lse, causal=False)
+            b.record()
+            torch.cuda.synchronize()
+            best.append(a.elapsed_time(b))
+        return min(best[1:])
+    small, large = time_of(50000), time_of(200000)
+    assert large < 8 * small, (small, large)
