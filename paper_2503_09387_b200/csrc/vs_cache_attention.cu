@@ -211,7 +211,7 @@ __global__ void __launch_bounds__(kThreads) cache_attention_few_kernel(const __g
             for (int n = 0; n < NT; ++n) mma_f16(sc[n][b], a0, a1, a2, a3, qf[n][4 * h + w][0], qf[n][4 * h + w][1]);
           }
         }
-      const int ev = exponent_of(scales.y);
+      const int ev = value_exponent(scales.y);
       const float evf = (float)ev, down = power_of_two(-ev);
       const bool edge = key0 < all_lo || key0 + kWarpKeys > all_hi;
       uint32_t pf[NT][2][2];
@@ -242,7 +242,7 @@ __global__ void __launch_bounds__(kThreads) cache_attention_few_kernel(const __g
           for (int j = 0; j < 2; ++j) {
             const float d = m_run[n][j] - m_new[j];
             r[j] = m_run[n][j] == -INFINITY ? 1.f : ex2_approx(d);
-            l_run[n][j] = m_run[n][j] == -INFINITY ? l_run[n][j] : times_power(l_run[n][j], d);
+            l_run[n][j] = m_run[n][j] == -INFINITY ? l_run[n][j] : moved_sum(l_run[n][j], d);
             m_run[n][j] = m_new[j];
           }
 #pragma unroll
@@ -250,19 +250,22 @@ __global__ void __launch_bounds__(kThreads) cache_attention_few_kernel(const __g
 #pragma unroll
             for (int j = 0; j < 4; ++j) o[n][i2][j] *= r[j & 1];
         }
+        if ((float)ev < -kSumTop)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) if (mx[j] - evf - m_run[n][j] > kSumTop) l_run[n][j] = shift_sum(l_run[n][j]);
         const float ref[2] = {m_run[n][0] == -INFINITY ? 0.f : m_run[n][0] - kLift, m_run[n][1] == -INFINITY ? 0.f : m_run[n][1] - kLift};
         float p[8];
         if (!__any_sync(0xffffffffu, far[0] || far[1])) {
 #pragma unroll
           for (int j = 0; j < 8; ++j) p[j] = ex2_approx(x[j] - ref[j & 1]);
 #pragma unroll
-          for (int j = 0; j < 2; ++j) l_run[n][j] = fmaf((p[j] + p[j + 2]) + (p[j + 4] + p[j + 6]), down, l_run[n][j]);
+          for (int j = 0; j < 2; ++j) l_run[n][j] = fmaf((p[j] + p[j + 2]) + (p[j + 4] + p[j + 6]), sum_factor(l_run[n][j], down), l_run[n][j]);
         } else {
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
             const int c = j & 1;
             p[j] = ex2_approx(x[j] - (far[c] ? mx[c] : ref[c]));
-            l_run[n][c] = fmaf(p[j], far[c] ? exp2f(mx[c] - ref[c] - evf) : down, l_run[n][c]);
+            l_run[n][c] = fmaf(p[j], sum_factor(l_run[n][c], far[c] ? exp2f(mx[c] - ref[c] - evf) : down), l_run[n][c]);
             if (far[c]) p[j] = 0.f;
           }
         }
@@ -314,10 +317,15 @@ __global__ void __launch_bounds__(kThreads) cache_attention_few_kernel(const __g
     for (int n = 0; n < NT; ++n)
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        float l = l_run[n][j];
-        l += __shfl_xor_sync(0xffffffffu, l, 4);
-        l += __shfl_xor_sync(0xffffffffu, l, 8);
-        l += __shfl_xor_sync(0xffffffffu, l, 16);
+        auto of_column = [&](float l) {
+          l += __shfl_xor_sync(0xffffffffu, l, 4);
+          l += __shfl_xor_sync(0xffffffffu, l, 8);
+          return l + __shfl_xor_sync(0xffffffffu, l, 16);
+        };
+        const bool wide = shifted(l_run[n][j]);
+        float l = of_column(l_run[n][j]);
+        if (__any_sync(0xffffffffu, wide))
+          l = chosen(of_column(wide ? -kSumUp * l_run[n][j] : l_run[n][j]), of_column(wide ? -l_run[n][j] : kSumDown * l_run[n][j]));
         const int col = 8 * n + 2 * q4 + j;
         if (g == 0) stats[warp * W + col] = make_float2(l == l ? m_run[n][j] : INFINITY, l);      // (NaN goes on as infinity - infinity)
         float* row = rows + (warp * W + col) * F::kRowF + (D / 8) * g;
@@ -335,6 +343,7 @@ __global__ void __launch_bounds__(kThreads) cache_attention_few_kernel(const __g
       for (int w = 0; w < kWarps; ++w) m = fmaxf(m, stats[w * W + col].x);
       float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
       float l = 0.f;
+      bool wide = false;
 #pragma unroll
       for (int w = 0; w < kWarps; ++w) {
         const float2 st = stats[w * W + col];
@@ -342,14 +351,25 @@ __global__ void __launch_bounds__(kThreads) cache_attention_few_kernel(const __g
         const float4 x = *reinterpret_cast<const float4*>(rows + (w * W + col) * F::kRowF + d);
         v.x = fmaf(f, x.x, v.x); v.y = fmaf(f, x.y, v.y); v.z = fmaf(f, x.z, v.z); v.w = fmaf(f, x.w, v.w);
         l += st.x == -INFINITY ? 0.f : times_power(st.y, st.x - m);
+        wide = wide || shifted(st.y);
+      }
+      if (wide) {
+        float by_2_64 = l = 0.f;
+#pragma unroll 1
+        for (int w = 0; w < kWarps; ++w) {
+          const float2 st = stats[w * W + col];
+          if (st.x == -INFINITY) continue;
+          l += as_is(st.y, st.x - m);
+          by_2_64 += as_shifted(st.y, st.x - m);
+        }
+        l = chosen(l, by_2_64);
       }
       if (part != nullptr) {
         *reinterpret_cast<float4*>(part + (size_t)col * D + d) = v;
         if (d == 0) part_stats<W, D>(a.parts, cta, begun ? 0 : 1)[col] = make_float2(m - kLift, l);
       } else {
-        const float inv = l == 0.f ? 0.f : 1.f / l;
         const RowHead to = row_head(a, s.first, r0 + col, it.head);
-        store_row_piece(a, to, d, make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv));
+        store_row_piece(a, to, d, times(v, reciprocal(l)));
         if (d == 0) store_lse(a, to, m - kLift, l);
       }
     }
@@ -365,6 +385,7 @@ struct JoinShared {
   int4 list[kFewCtas];                  // what the last CTA of an item noted
   int last[kFewCtas], count[(kFewCtas + 31) / 32];
   float2 st[kJoinWarps];
+  int wide[kJoinWarps];                 // whether a warp met a sum that is held times 2^-64
   float4 o[kJoinWarps][32];
 };
 // Parts of a row, up to 32 side by side: a lane knows one's reference and sum (on: there is one), and has four dims of each, which `get` gives
@@ -411,6 +432,21 @@ __device__ __forceinline__ void add_part(Sum& s, float2 st, float4 v) {
   s.l = (s.m == -INFINITY ? 0.f : times_power(s.l, s.m - m)) + times_power(st.y, st.x - m);
   s.m = m;
 }
+// l of a row of which a part's sum is held times 2^-64, by a warp: m is the largest reference of CTAs first ... last.  (Apart from the rest, which
+// knows of none: 0.5 us of a question's join otherwise.)
+template <int W, int D>
+__device__ __noinline__ float sum_of_parts(float* parts, int first, int last, int col, float m) {
+  float l = 0.f, by_2_64 = 0.f;
+  for (int c = first + (int)(threadIdx.x & 31); c <= last; c += 32) {
+    const float2 st = part_stats<W, D>(parts, c, c == first ? 1 : 0)[col];
+    if (st.x == -INFINITY) continue;
+    l += as_is(st.y, st.x - m);
+    by_2_64 += as_shifted(st.y, st.x - m);
+  }
+#pragma unroll
+  for (int k = 16; k > 0; k >>= 1) { l += __shfl_xor_sync(0xffffffffu, l, k); by_2_64 += __shfl_xor_sync(0xffffffffu, by_2_64, k); }
+  return chosen(l, by_2_64);
+}
 // The items that a kernel's CTAs left in parts, by all blocks: a block lists the CTAs that were the last on an item others had begun.  Where
 // these are many, and so of few parts each, it takes eight columns of an item at a time, a warp to each; else one, its parts shared by the warps.
 // (Sixteen items of two parts, 224 columns: 7 us more column by column.  Four of 36 parts: 8 us, 16.5 MB of parts.)
@@ -440,9 +476,8 @@ __device__ __forceinline__ void join_items(const CacheAttnArgs& a, const int4* j
   }
   __syncthreads();
   auto finish = [&](const int4& j, int col, float m, float l, const float4& o) {
-    const float inv = l == 0.f ? 0.f : 1.f / l;
     const RowHead to = row_head(a, j.y, j.z + col, j.w & 0xffff);
-    if (lane < D / 4) store_row_piece(a, to, 4 * lane, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
+    if (lane < D / 4) store_row_piece(a, to, 4 * lane, times(o, reciprocal(l)));
     if (lane == 0) store_lse(a, to, m, l);
   };
   if constexpr (W >= 8 * kJoinWarps) {
@@ -456,6 +491,7 @@ __device__ __forceinline__ void join_items(const CacheAttnArgs& a, const int4* j
         Sum s[P];
 #pragma unroll
         for (int p = 0; p < P; ++p) s[p] = {-INFINITY, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
+        bool wide = false;
 #pragma unroll 1
         for (int c0 = first; c0 <= last; c0 += U) {
           float2 st[U][P];
@@ -472,8 +508,10 @@ __device__ __forceinline__ void join_items(const CacheAttnArgs& a, const int4* j
 #pragma unroll
           for (int i = 0; i < U; ++i)
 #pragma unroll
-            for (int p = 0; p < P; ++p) add_part(s[p], st[i][p], v[i][p]);
+            for (int p = 0; p < P; ++p) { add_part(s[p], st[i][p], v[i][p]); wide = wide || shifted(st[i][p].y); }
         }
+#pragma unroll
+        for (int p = 0; p < P; ++p) if (wide) s[p].l = sum_of_parts<W, D>(parts, first, last, col0 + p, s[p].m);
 #pragma unroll
         for (int p = 0; p < P; ++p) if (col0 + p < (j.w >> 16)) finish(j, col0 + p, s[p].m, s[p].l, s[p].o);
       }
@@ -487,25 +525,29 @@ __device__ __forceinline__ void join_items(const CacheAttnArgs& a, const int4* j
     if (col >= (j.w >> 16)) continue;                      // (the whole block)
     float m = -INFINITY, l = 0.f;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    bool wide = false;
 #pragma unroll 1
     for (int c0 = first + warp; c0 <= last; c0 += 32 * kJoinWarps) {
       const int n = min(32, (last - c0) / kJoinWarps + 1);
       auto place = [&](int c) { return c == first ? 1 : 0; };
       const int mine = c0 + min(lane, n - 1) * kJoinWarps;
       const float2 st = part_stats<W, D>(parts, mine, place(mine))[col];
+      wide = wide || shifted(st.y);
       join_parts(n, lane < n, st, m, l, o, [&](int i) {
         const int c = c0 + i * kJoinWarps;
         return lane < D / 4 ? *reinterpret_cast<const float4*>(part_rows<W, D>(parts, c, place(c)) + (size_t)col * D + 4 * lane) : make_float4(0.f, 0.f, 0.f, 0.f);
       });
     }
     __syncthreads();                                        // (the round before has been read)
-    if (lane == 0) sm.st[warp] = make_float2(m, l);
+    wide = __any_sync(0xffffffffu, wide);
+    if (lane == 0) { sm.st[warp] = make_float2(m, l); sm.wide[warp] = wide; }
     sm.o[warp][lane] = o;
     __syncthreads();
     if (warp != 0) continue;
     m = -INFINITY;
     o = make_float4(0.f, 0.f, 0.f, 0.f);
     join_parts(kJoinWarps, lane < kJoinWarps, sm.st[lane & (kJoinWarps - 1)], m, l, o, [&](int i) { return sm.o[i][lane]; });
+    if (__any_sync(0xffffffffu, sm.wide[lane & (kJoinWarps - 1)] != 0)) l = sum_of_parts<W, D>(parts, first, last, col, m);
     finish(j, col, m, l, o);
   }
 }

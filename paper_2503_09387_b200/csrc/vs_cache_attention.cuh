@@ -218,12 +218,31 @@ __device__ __forceinline__ float* part_rows(float* parts, int cta, int place) { 
 template <int W, int D>
 __device__ __forceinline__ float2* part_stats(float* parts, int cta, int place) { return reinterpret_cast<float2*>(part_rows<W, D>(parts, cta, place) + (size_t)W * D); }
 
-// A row's sum l goes by the scores alone and its reference m by score and page exponent: with pages whose exponents lie 230 apart 2^d, d <= 0, may
-// be nothing where l 2^d is not.  In two halves.
-__device__ __forceinline__ float times_power(float l, float d) {
+// A row's sum l goes by the scores alone and its reference m by score and page exponent: l = sum of 2^{x - m + lift - ev}, where a page's exponent ev is
+// anything from -110 (values of nothing but zeros) to 120.  The low end fits fp32: all of l is 2^-113 at the least, and what counts beside that 2^-137.  The high end
+// does not, 2^125 a key.  So a sum is held times 2^-64 from the first page on whose largest score lies 70 above m, and has its sign set to say so; as it is
+// again once it would be small that way.  Either way 2^31 keys are far from an overflow and nothing that counts is lost, and pages of usual exponents pay
+// a comparison.  (Held in fp64: frames 182 -> 192 us.)
+constexpr float kSumTop = 70.f, kSumShift = 64.f, kSumDown = 0x1p-64f, kSumUp = 0x1p64f;
+__device__ __forceinline__ bool shifted(float l) { return __float_as_int(l) < 0; }
+__device__ __forceinline__ int value_exponent(float scale) { return max(exponent_of(scale), kScaleMinExp); }      // (a scale of 0 belongs to zeros)
+__device__ __forceinline__ float times_power(float l, float d) {          // in two halves: 2^d, d <= 0, may be nothing where l 2^d is not
   const float h = exp2f(0.5f * d);
   return l * h * h;
 }
+__device__ __forceinline__ float sum_factor(float l, float down) { return shifted(l) ? -kSumDown * down : down; }      // of a page's weights, to be added to l
+__device__ __forceinline__ float shift_sum(float l) { return shifted(l) ? l : -kSumDown * l; }
+__device__ __forceinline__ float moved_sum(float l, float d) {            // for a reference that moved by -d
+  if (shifted(l) && l * exp2f(d) > -1e-6f) { l = -l; d += kSumShift; }
+  return times_power(l, d);
+}
+// A sum of sums, where any of them is held times 2^-64: added up as they are and all times 2^-64, and chosen.
+__device__ __forceinline__ float as_is(float l, float d) { return shifted(l) ? times_power(-l, d + kSumShift) : times_power(l, d); }
+__device__ __forceinline__ float as_shifted(float l, float d) { return shifted(l) ? times_power(-l, d) : times_power(l, d - kSumShift); }
+__device__ __forceinline__ float chosen(float l, float by_2_64) { return l < 0x1p60f ? l : -by_2_64; }
+// 1 / l as two factors; 0 of 0 (a row that sees nothing)
+__device__ __forceinline__ float2 reciprocal(float l) { return make_float2(l == 0.f ? 0.f : 1.f / fabsf(l), shifted(l) ? kSumDown : 1.f); }
+__device__ __forceinline__ float4 times(float4 v, float2 by) { return make_float4(v.x * by.x * by.y, v.y * by.x * by.y, v.z * by.x * by.y, v.w * by.x * by.y); }
 constexpr float kFar = 40.f;      // a page whose largest x lies as far below m adds nothing to a row's O; to its l perhaps
 
 // place in [n_rows][Hq] of packed row r (of a sequence whose rows begin at `first`) of KV head h: row and head
@@ -241,7 +260,13 @@ __device__ __forceinline__ void store_row_piece(const CacheAttnArgs& a, RowHead 
   }
 }
 __device__ __forceinline__ void store_lse(const CacheAttnArgs& a, RowHead p, float m, float l) {
-  if (a.lse != nullptr) a.lse[(long long)p.row * a.Hq + p.head] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+  if (a.lse == nullptr) return;
+  float log2_l = m + log2f(l);
+  if (shifted(l)) {                    // (the whole powers of two to m first, which undo one another: some 2^70, -125)
+    const float x = -l, e = (float)exponent_of(x);
+    log2_l = (m + (e + kSumShift)) + log2f(x * exp2f(-e));
+  }
+  a.lse[(long long)p.row * a.Hq + p.head] = l == 0.f ? -INFINITY : log2_l * 0.6931471805599453f;
 }
 #endif
 

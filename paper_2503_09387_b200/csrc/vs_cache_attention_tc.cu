@@ -400,7 +400,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attention_tc_kernel(const _
         }
         const int key0 = (it.page + p) * kPage;
         const float f = fmaxf(factor * __shfl_sync(0xffffffffu, ks_mine, p & 31), 1.2e-38f);      // (0 would make NaN of a hidden key's -inf)
-        const int ev = exponent_of(__shfl_sync(0xffffffffu, vs_mine, p & 31));
+        const int ev = value_exponent(__shfl_sync(0xffffffffu, vs_mine, p & 31));
         const bool there = __shfl_sync(0xffffffffu, there_mine, p & 31) != 0;
         const bool edge = __any_sync(0xffffffffu, !there || seen.lo > key0 || seen.hi < key0 + kPage);
         const float evf = (float)ev;
@@ -442,7 +442,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attention_tc_kernel(const _
         if (rare) {
           float alpha = 1.f;
           if (moves) {
-            if (m_run > -INFINITY) { alpha = exp2f(m_run - most); l_run = times_power(l_run, m_run - most); }
+            if (m_run > -INFINITY) { alpha = exp2f(m_run - most); l_run = moved_sum(l_run, m_run - most); }
             m_run = most;
             ref = kLift - most;
           }
@@ -463,6 +463,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attention_tc_kernel(const _
             }
           }
         }
+        if (evf < -kSumTop && some && most - evf - m_run > kSumTop) l_run = shift_sum(l_run);
         const uint64_t f2 = f32x2(f, f), c2 = f32x2(shift, shift);
         uint64_t sum[2] = {0ull, 0ull};
 #pragma unroll
@@ -483,7 +484,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attention_tc_kernel(const _
           tmem_st_row16(tp + 16u * (uint32_t)q, pw);
         }
         const float2 s2 = f32x2_parts(add_f32x2(sum[0], sum[1]));
-        if (some) l_run = fmaf(s2.x + s2.y, down, l_run);
+        if (some) l_run = fmaf(s2.x + s2.y, sum_factor(l_run, down), l_run);
         tmem_st_wait();
         tc_fence_before();
         __syncwarp();
@@ -501,7 +502,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attention_tc_kernel(const _
         else part_stats<kWide, D>(a.parts, cta, begun ? 0 : 1)[col] = make_float2(m_run - kLift, l_run);
       }
       // a quad of lanes to two rows: where they go, as fp32 (parts always) or bf16
-      const float mul = whole ? (l_run == 0.f ? 0.f : 1.f / l_run) : 1.f;
+      const float2 mul = whole ? reciprocal(l_run) : make_float2(1.f, 1.f);
       const bool fp32 = !whole || a.out_fp32;
       char* const to_base = whole ? static_cast<char*>(a.out) : reinterpret_cast<char*>(part_rows<kWide, D>(a.parts, cta, begun ? 0 : 1));
       const long long to_row = (whole ? (long long)rh.row * a.out_row + (long long)rh.head * a.out_head : (long long)col * D) * (fp32 ? 4 : 2);
@@ -514,15 +515,15 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attention_tc_kernel(const _
         tmem_ld_wait();
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
-          const float m = __shfl_sync(0xffffffffu, mul, r0 + 8 * half);
+          const float m = __shfl_sync(0xffffffffu, mul.x, r0 + 8 * half), m2 = __shfl_sync(0xffffffffu, mul.y, r0 + 8 * half);
           char* dst = to_base + __shfl_sync(0xffffffffu, to_row, r0 + 8 * half) + (c + 2 * (lane & 3)) * (fp32 ? 4 : 2);
           if (i * kRows + 32 * quarter + r0 + 8 * half >= it.n_cols) continue;
           if (fp32) {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) *reinterpret_cast<float2*>(dst + 32 * k) = make_float2(v[4 * k + 2 * half] * m, v[4 * k + 2 * half + 1] * m);
+            for (int k = 0; k < 8; ++k) *reinterpret_cast<float2*>(dst + 32 * k) = make_float2(v[4 * k + 2 * half] * m * m2, v[4 * k + 2 * half + 1] * m * m2);
           } else {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) *reinterpret_cast<uint32_t*>(dst + 16 * k) = pack2(v[4 * k + 2 * half] * m, v[4 * k + 2 * half + 1] * m);
+            for (int k = 0; k < 8; ++k) *reinterpret_cast<uint32_t*>(dst + 16 * k) = pack2(v[4 * k + 2 * half] * m * m2, v[4 * k + 2 * half + 1] * m * m2);
           }
         }
       }
