@@ -567,9 +567,9 @@ int few_ctas(int cols) { return cols <= 8 ? kFewCtas : 2 * 148; }
 template <int D, int NT>
 int launch_few(const CacheAttnArgs& a, cudaStream_t st) {
   using F = Few<D, NT>;
-  const int bytes = F::bytes(a.r.n_seqs);
-  if (cudaFuncSetAttribute(cache_attention_few_kernel<D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return VS_ERR_CUDA;
-  cache_attention_few_kernel<D, NT><<<few_ctas(8 * NT), kThreads, bytes, st>>>(a);
+  // (the limit is the function's, not the call's: that of the most sequences, so that calls of other threads set the same)
+  if (cudaFuncSetAttribute(cache_attention_few_kernel<D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, F::bytes(VS_CACHE_MAX_SEQS)) != cudaSuccess) return VS_ERR_CUDA;
+  cache_attention_few_kernel<D, NT><<<few_ctas(8 * NT), kThreads, F::bytes(a.r.n_seqs), st>>>(a);
   return launched();
 }
 

@@ -46,7 +46,7 @@ struct Tc {
   static constexpr int kSlotWord = kFlags + 8 * kRing;
   static constexpr int kPlaces = (kSlotWord + 8 + 15) / 16 * 16;               // [warp] where its last item lies
   static constexpr int kBefore = kPlaces + 16 * (kThreads / 32);
-  static int bytes(int n_seqs) { return kBefore + 8 * (n_seqs + 1 + kCutWords); }
+  static constexpr int bytes(int n_seqs) { return kBefore + 8 * (n_seqs + 1 + kCutWords); }
 };
 
 // The page tiles of an item of n pages in the order of their use: K(0), K(1), V(0), K(2), V(1), ... K(n - 1), V(n - 2), V(n - 1)
@@ -543,13 +543,13 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attention_tc_kernel(const _
 
 template <int D>
 int launch_tc(const CacheAttnArgs& a, bool behind_few, cudaStream_t st) {
-  const int bytes = Tc<D>::bytes(a.r.n_seqs);
-  static_assert(Tc<D>::kBefore + 8 * (VS_CACHE_MAX_SEQS + 1 + kCutWords) <= 227 * 1024, "shared memory of an SM");
-  if (cudaFuncSetAttribute(cache_attention_tc_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return VS_ERR_CUDA;
+  static_assert(Tc<D>::bytes(VS_CACHE_MAX_SEQS) <= 227 * 1024, "shared memory of an SM");
+  // (the limit is the function's, not the call's: that of the most sequences, so that calls of other threads set the same)
+  if (cudaFuncSetAttribute(cache_attention_tc_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, Tc<D>::bytes(VS_CACHE_MAX_SEQS)) != cudaSuccess) return VS_ERR_CUDA;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(kManyCtas);
   cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = (size_t)bytes;
+  cfg.dynamicSmemBytes = (size_t)Tc<D>::bytes(a.r.n_seqs);
   cfg.stream = st;
   cudaLaunchAttribute at = {};
   at.id = cudaLaunchAttributeProgrammaticStreamSerialization;      // (other rows, other parts of the workspace: nothing to wait for but its end)
