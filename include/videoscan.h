@@ -387,7 +387,8 @@ int vs_cache_read(const vs_cache* cache, const vs_cache_rows* rows, void* cuda_s
  *      with those over other keys (the bank's, say) takes.
  * scale: of the scores, usually 1 / sqrt(head_dim).
  * workspace: DEVICE, at least vs_cache_attention_bytes, 256-byte aligned; its contents need not be kept
- *      between calls, but no two calls that may overlap can share it.  Its first int32 becomes
+ *      between calls, but no two calls that may overlap can share it (calls of two host threads on one stream
+ *      do: a call is several launches).  Its first int32 becomes
  *      VS_ERR_DEVICE_TIMEOUT if a bounded wait of a kernel expires (the call's rows are unspecified then) and is
  *      written in no other case: clear it once. */
 int vs_cache_attention_bytes(int32_t head_dim, size_t* out_bytes);

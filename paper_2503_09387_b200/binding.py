@@ -11,6 +11,7 @@ from __future__ import annotations
 import ctypes as C
 import os
 import struct
+import threading
 from typing import List, Optional, Sequence
 
 import numpy as np
@@ -405,6 +406,7 @@ class PageCache:
         self._cache = VsCache(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), self.n_pages, self.n_kv_heads,
                               self.head_dim, self.device_index)
         self._workspaces = {}
+        self._attending = threading.Lock()           # a call is several launches, and two calls' may not mix on one workspace
 
     @classmethod
     def empty(cls, n_pages: int, n_kv_heads: int, head_dim: int, device=0) -> "PageCache":
@@ -469,7 +471,7 @@ class PageCache:
         """Attention of q bf16 [n_rows, n_q_heads, head_dim] over each sequence's ``lengths[i]`` tokens, its rows counted in.
         -> (out [n_rows, n_q_heads, head_dim], lse fp32 [n_rows, n_q_heads]).  ``out_dtype``: of a new ``out``, bf16 or fp32.  Without
         ``workspace`` the cache keeps one for every stream it is used on; a call that is captured takes one from the graph's own memory, so
-        that graphs replayed side by side share none (its status is then nobody's to read)."""
+        that graphs replayed side by side share none (its status is then nobody's to read).  Several host threads may call it, on one stream too."""
         torch, index = _torch, self.device_index
         shape, step = q.shape, q.stride()
         _need(len(shape) == 3 and q.dtype is torch.bfloat16 and shape[2] == self.head_dim and step[2] == 1 and q.get_device() == index,
@@ -483,20 +485,22 @@ class PageCache:
         _need(out.shape == shape and out_step[2] == 1 and out.get_device() == index, "attend: out like q")
         _need(lse.numel() == n_rows * n_heads and lse.dtype is torch.float32 and lse.is_contiguous() and lse.get_device() == index,
               "attend: lse fp32 [n_rows, n_q_heads]")
+        seqs = self._seqs(page_table, lengths, row_offsets)
+        code = _dtype_code(out.dtype, "attend: out of bf16 or fp32 wanted")
+        _need(workspace is None or workspace.is_contiguous() and workspace.get_device() == index, "attend: a workspace on the cache's GPU")
         stream = _raw_stream(index)
-        if workspace is None:
-            if _capturing(index):
-                workspace = self._new_workspace()
-            else:
-                workspace = self._workspaces.get(stream)
-                if workspace is None:
-                    workspace = self._workspaces[stream] = self.workspace()
-        else:
-            _need(workspace.is_contiguous() and workspace.get_device() == index, "attend: a workspace on the cache's GPU")
-        block = VS_CACHE_QUERIES.pack(*self._seqs(page_table, lengths, row_offsets), n_rows, 0, q.data_ptr(), out.data_ptr(), lse.data_ptr(),
-                                      workspace.data_ptr(), workspace.nbytes, step[0], step[1], out_step[0], out_step[1], n_heads, causal, window,
-                                      _dtype_code(out.dtype, "attend: out of bf16 or fp32 wanted"), head_dim ** -0.5 if scale is None else scale, 0)
-        _check(load_library().vs_cache_attention(self._cache, block, stream), "vs_cache_attention")
+        with self._attending:
+            if workspace is None:
+                if _capturing(index):
+                    workspace = self._new_workspace()
+                else:
+                    workspace = self._workspaces.get(stream)
+                    if workspace is None:
+                        workspace = self._workspaces[stream] = self.workspace()
+            block = VS_CACHE_QUERIES.pack(*seqs, n_rows, 0, q.data_ptr(), out.data_ptr(), lse.data_ptr(), workspace.data_ptr(), workspace.nbytes,
+                                          step[0], step[1], out_step[0], out_step[1], n_heads, causal, window, code,
+                                          head_dim ** -0.5 if scale is None else scale, 0)
+            _check(load_library().vs_cache_attention(self._cache, block, stream), "vs_cache_attention")
         return out, lse
 
 

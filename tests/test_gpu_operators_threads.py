@@ -57,3 +57,27 @@ def test_attend_of_few_and_of_most_sequences_in_two_threads(rows):
                 assert same_bits(out, want[0]) and same_bits(lse, want[1])
         return f
     run_threads([many(*c) for c in calls for _ in range(2)])
+
+
+@pytest.mark.parametrize("rows", [(1, 3), (40, 70), (1, 40)])
+def test_attend_from_two_threads_on_one_stream(rows):
+    """One cache, one stream and so one workspace: the launches of two calls do not mix."""
+    g = gen(9)
+    cache = pool(g, 200, 4, 128, junk=False)
+    calls = []
+    for n, length in zip(rows, (6000, 2900)):
+        table, q = tables(g, [length], 200), normal(g, n, 28, 128)
+        calls.append((table, ints([length]), q, cache.attend(table, ints([length]), q)))
+    stream = torch.cuda.Stream()
+    torch.cuda.synchronize()
+
+    def many(table, lengths, q, want):
+        def f():
+            with torch.cuda.stream(stream):
+                got = [cache.attend(table, lengths, q) for _ in range(200)]
+                stream.synchronize()
+                for out, lse in got:
+                    assert same_bits(out, want[0]) and same_bits(lse, want[1])
+        return f
+    run_threads([many(*c) for c in calls])
+    assert cache.attend_status() == 0
