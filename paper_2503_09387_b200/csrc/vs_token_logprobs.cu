@@ -481,8 +481,9 @@ extern "C" int vs_token_logprobs(const vs_scores* x, void* cuda_stream) {
   if (x == nullptr || x->rows < 0 || x->vocab < 1 || x->dtype < 0 || x->dtype > 1 || x->top < 0) return VS_ERR_INVALID_ARG;
   if (x->vocab > (1 << 30) || x->rows > (1 << 27)) return VS_ERR_UNSUPPORTED;
   if (x->top > VS_MAX_TOP) return VS_ERR_CAPACITY;
-  if (x->top > x->vocab || (x->top > 0 && x->top_index == nullptr)) return VS_ERR_INVALID_ARG;
+  if (x->top > x->vocab) return VS_ERR_INVALID_ARG;
   if (x->rows == 0) return VS_OK;
+  if (x->top > 0 && x->top_index == nullptr) return VS_ERR_INVALID_ARG;
   if ((x->logprob != nullptr || x->rank != nullptr) && x->tokens == nullptr) return VS_ERR_INVALID_ARG;
   const size_t el = x->dtype == 1 ? 4 : 2;
   if (x->logits == nullptr || !aligned(x->logits, el)) return VS_ERR_INVALID_ARG;

@@ -129,3 +129,11 @@ def test_refusals_of_outputs_over_inputs(lib):
     c = binding.VsCache(**CACHE)
     for change in (dict(outh=256), dict(outr=128), dict(dtype=1)):
         assert lib.vs_cache_attention(c, queries(**change), None) == INVALID, change
+
+
+def test_token_logprobs_of_no_rows(lib):
+    """Nothing is asked for, whatever the number of alternatives: the outputs are empty and have no address."""
+    none = dict(logits=0, tokens=0, lp=0, entropy=0, rank=0, best=0, best_lp=0, stride=1000, dtype=1, rows=0, vocab=1000, top=5, device=0, reserved=0)
+    assert lib.vs_token_logprobs(binding.VS_SCORES.pack(*none.values()), None) == 0
+    for change, code in ((dict(top=33), CAPACITY), (dict(vocab=4), INVALID), (dict(top=-1), INVALID)):
+        assert lib.vs_token_logprobs(binding.VS_SCORES.pack(*dict(none, **change).values()), None) == code, change
