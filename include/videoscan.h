@@ -376,7 +376,7 @@ int vs_cache_read(const vs_cache* cache, const vs_cache_rows* rows, void* cuda_s
 /* Softmax attention of each sequence's rows over its tokens in the cache (Eq. 1, grouped KV heads):
  * row j of n stands at position tokens - n + j and sees the tokens that exist, with causal != 0 none
  * behind itself, with window > 0 only the last `window` up to itself.  A row that sees nothing gets zeros
- * (and -inf in lse).  Tokens that no row of the call sees may hold anything.
+ * (and -inf in lse).  Tokens that a row does not see may hold anything, NaN too; a NaN value that it sees is its own in that element.
  * q:   DEVICE bf16 [n_rows][n_q_heads][head_dim], 16-byte aligned, strides multiples of 8;
  *      n_q_heads % n_kv_heads == 0, at most 8 query heads a KV head.
  *      Several sequences may name the same page, and one may name it several times.

@@ -169,6 +169,8 @@ __global__ void __launch_bounds__(kThreads) cache_attention_few_kernel(const __g
     all_lo = __reduce_max_sync(0xffffffffu, all_lo); all_hi = __reduce_min_sync(0xffffffffu, all_hi);
     any_lo = __reduce_min_sync(0xffffffffu, any_lo); any_hi = __reduce_max_sync(0xffffffffu, any_hi);
 
+    const bool uneven = any_lo < all_lo || all_hi < any_hi;
+
     float o[NT][KS][4];              // O^T: tile m of 16 dims; rows g -> (D / 8) g + 2 m, g + 8 -> that + 1; columns 2 q4, 2 q4 + 1
     float m_run[NT][2], l_run[NT][2];
 #pragma unroll
@@ -293,6 +295,48 @@ __global__ void __launch_bounds__(kThreads) cache_attention_few_kernel(const __g
           if (edge && (key0 + r >= any_hi || key0 + r < any_lo))
 #pragma unroll
             for (int w = 0; w < D / 32; ++w) vw[j][w] = 0u;
+        }
+        // what some columns see and others do not: its NaN goes to those that do
+        if (edge && uneven) {
+          uint32_t nan = 0u;
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int w = 0; w < D / 32; ++w) nan |= nan_codes(vw[j][w]);
+          if (__any_sync(0xffffffffu, nan != 0u)) {
+            // ... by a product of its own, of ones: NaN's codes times the keys that a column sees
+            uint32_t sf[NT][2];
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+              for (int k = 0; k < 2; ++k) {
+                const int key = key0 + 16 * b + g + 8 * k;
+                sf[n][k] = transpose_8x8(half2_of(key >= lo_of[n][0] && key < hi_of[n][0] ? 1.f : 0.f, key >= lo_of[n][1] && key < hi_of[n][1] ? 1.f : 0.f));
+              }
+#pragma unroll
+            for (int w = 0; w < D / 32; ++w) {
+              uint32_t one[4];
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                const uint32_t at_nan = nan_codes(vw[j][w]);
+                one[j] = at_nan * 0x38u;                     // (the code of 1)
+                vw[j][w] &= ~(at_nan * 0xffu);
+              }
+#pragma unroll
+              for (int hh = 0; hh < 2; ++hh) {
+                uint32_t a0, a1, a2, a3;
+                codes_to_half2(__byte_perm(one[0], one[1], hh ? 0x7362 : 0x5140), a0, a1);
+                codes_to_half2(__byte_perm(one[2], one[3], hh ? 0x7362 : 0x5140), a2, a3);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                  float c[4] = {0.f, 0.f, 0.f, 0.f};
+                  mma_f16(c, a0, a1, a2, a3, sf[n][0], sf[n][1]);
+#pragma unroll
+                  for (int k = 0; k < 4; ++k) if (c[k] > 0.f) o[n][2 * w + hh][k] = __int_as_float(0x7fc00000);
+                }
+              }
+            }
+          }
         }
 #pragma unroll
         for (int w = 0; w < D / 32; ++w)

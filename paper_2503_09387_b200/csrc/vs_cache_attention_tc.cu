@@ -42,9 +42,10 @@ struct Tc {
   static constexpr int kQTile = kRows * D * 2, kTile = kPage * D * 2, kRawTile = kPage * D;
   static constexpr int kQ = 0, kF16 = kTiles * kQTile, kRawAt = kF16 + kRing * kTile, kCtl = kRawAt + kRing * kRawTile;
   static constexpr int kBars = 4 * kRing + 7 * kTiles;
-  static constexpr int kFlags = kCtl + 8 * kBars;       // [place] first and end of the rows of the raw tile that count (end 0: the page is not there)
+  static constexpr int kFlags = kCtl + 8 * kBars;       // [place] first and end of the rows of the raw tile that count (end 0: the page is not there); 256 in the first: values that not all rows of the item see alike
   static constexpr int kSlotWord = kFlags + 8 * kRing;
-  static constexpr int kPlaces = (kSlotWord + 8 + 15) / 16 * 16;               // [warp] where its last item lies
+  static constexpr int kNanWord = kSlotWord + 8;        // whether a value that only some rows of an item see was NaN
+  static constexpr int kPlaces = (kNanWord + 4 + 15) / 16 * 16;               // [warp] where its last item lies
   static constexpr int kBefore = kPlaces + 16 * (kThreads / 32);
   static constexpr int bytes(int n_seqs) { return kBefore + 8 * (n_seqs + 1 + kCutWords); }
 };
@@ -107,6 +108,58 @@ __device__ __forceinline__ uint4 lds128(uint32_t addr) {
   return v;
 }
 
+// Keys that any row of an item sees, and that all of them do.  (Both ends go up with the row.)
+constexpr int kUneven = 256;
+struct ItemKeys {
+  int any_lo, all_lo, all_hi, any_hi;
+  // of a page: whether rows see different ones of its keys
+  __device__ __forceinline__ bool uneven(int key0) const { return (any_lo < all_lo && key0 < all_lo) || (all_hi < any_hi && key0 > all_hi - kPage); }
+};
+__device__ __forceinline__ ItemKeys keys_of_item(const CacheAttnArgs& a, const AttnItem& it) {
+  const KeyRange first = keys_of(a, it.s, by_group(a, it.r0)), last = keys_of(a, it.s, by_group(a, it.r0 + it.n_cols - 1));
+  return {first.lo, last.lo, first.hi, last.hi};
+}
+
+// The NaN of values that some rows of an item see and others do not.  The converters put zeros in their place; here, once the last product is
+// complete, every thread sets to NaN the dims of its row of O whose NaN the row sees.  It reads the pages in question once more.
+template <int D>
+__device__ __forceinline__ void set_seen_nan(const CacheAttnArgs& a, ItemKeys keys, int seq, int head, int page0, int n_pages, KeyRange seen, uint32_t to) {
+  uint32_t dims[D / 32];
+#pragma unroll
+  for (int w = 0; w < D / 32; ++w) dims[w] = 0u;
+  for (int p = page0; p < page0 + n_pages; ++p) {
+    const int key0 = p * kPage;
+    if (!keys.uneven(key0)) continue;
+    const int page = page_of(a.r, a.c.n_pages, seq, p);
+    if (page < 0) continue;
+    const uint8_t* const from = static_cast<const uint8_t*>(a.c.v) + ((size_t)page * a.c.n_kv_heads + head) * (size_t)(kPage * D);
+    for (int k = max(seen.lo - key0, 0); k < min(seen.hi - key0, kPage); ++k)
+#pragma unroll
+      for (int w = 0; w < D / 32; ++w)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const uint4 v = *reinterpret_cast<const uint4*>(from + k * D + 32 * w + 16 * h);
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            const uint32_t n = nan_codes(word(v, c));
+            dims[w] |= ((n | n >> 7 | n >> 14 | n >> 21) & 15u) << (16 * h + 4 * c);
+          }
+        }
+  }
+#pragma unroll 1
+  for (int c = 0; c < D; c += 16) {
+    uint32_t o[16], set = 0u;
+#pragma unroll
+    for (int w = 0; w < D / 32; ++w) if (c / 32 == w) set = dims[w] >> (c & 31);
+    __syncwarp();
+    tmem_ld_row16(to + (uint32_t)c, o);
+#pragma unroll
+    for (int k = 0; k < 16; ++k) if (set >> k & 1u) o[k] = 0x7fc00000u;
+    tmem_st_row16(to + (uint32_t)c, o);
+  }
+  tmem_st_wait();
+}
+
 template <int D>
 __global__ void __launch_bounds__(kThreads, 1) cache_attention_tc_kernel(const __grid_constant__ CacheAttnArgs a) {
   using L = Tc<D>;
@@ -127,6 +180,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attention_tc_kernel(const _
   volatile int2* flags = reinterpret_cast<volatile int2*>(smem + L::kFlags);
   volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(smem + L::kSlotWord);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + L::kSlotWord + 4);
+  volatile int* nan_flag = reinterpret_cast<volatile int*>(smem + L::kNanWord);
   long long* before = reinterpret_cast<long long*>(smem + L::kBefore);
   ItemPlace* const place_of = reinterpret_cast<ItemPlace*>(smem + L::kPlaces) + warp;
 
@@ -134,6 +188,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attention_tc_kernel(const _
   if (warp == kIssuerWarp) {
     for (uint32_t x = (uint32_t)lane; x < (uint32_t)L::kBars; x += 32u)
       mbar_init(ctl + 8u * x, (x >= kRing && x < 3 * kRing) || (x >= kTileBars && x < kTileBars + 3 * kTiles) ? 4u : (x >= 3 * kRing && x < 4 * kRing ? 2u : 1u));       // (converters, softmax: four warps; issuers: two)
+    if (lane == 0) *nan_flag = 0;
     if (lane == 0) *abort_flag = (base & 1023u) != 0;     // (the swizzled layouts need the alignment that the declaration asks for)
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_async_proxy();
@@ -160,8 +215,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attention_tc_kernel(const _
         const AttnItem it = item_at<kWide>(a, before, runs, u, u_end, place_of);
         if (it.n < 1) break;
         u += it.span;
-        // keys that any row of the item sees
-        const int lo = keys_of(a, it.s, by_group(a, it.r0)).lo, hi = keys_of(a, it.s, by_group(a, it.r0 + it.n_cols - 1)).hi;
+        const ItemKeys seen = keys_of_item(a, it);
         uint32_t place = (done + (uint32_t)lane) % kRing, phase = ((done + (uint32_t)lane) / kRing + 1u) & 1u;      // (phase: of bar_raw_free, before this use)
         int p = page_of_tile(lane, it.n), page = lane < 4 && lane < 2 * it.n ? page_of(a.r, a.c.n_pages, it.seq, it.page + p) : -1;
         for (int e0 = 0; e0 < 2 * it.n && ok; e0 += 4) {
@@ -172,7 +226,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attention_tc_kernel(const _
             const uint8_t* const from = static_cast<const uint8_t*>(is_v ? a.c.v : a.c.k) + ((size_t)max(page, 0) * a.c.n_kv_heads + it.head) * (size_t)L::kRawTile;
             ok = mbar_wait(bar_raw_free(place), phase, abort_flag);
             if (ok) {
-              const_cast<int2*>(flags)[place] = page >= 0 ? make_int2(max(min(lo - key0, kPage), 0), max(min(hi - key0, kPage), 0)) : make_int2(0, 0);
+              const_cast<int2*>(flags)[place] = page >= 0 ? make_int2(max(min(seen.any_lo - key0, kPage), 0) + (is_v && seen.uneven(key0) ? kUneven : 0), max(min(seen.any_hi - key0, kPage), 0)) : make_int2(0, 0);
               if (page >= 0) {
                 mbar_arrive_expect_tx(bar_raw_full(place), (uint32_t)L::kRawTile);
                 bulk_load(base + L::kRawAt + place * (uint32_t)L::kRawTile, from, (uint32_t)L::kRawTile, bar_raw_full(place));
@@ -287,7 +341,9 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attention_tc_kernel(const _
       for (; x < end; x += 2u) {
         const uint32_t place = x % kRing, phase = (x / kRing) & 1u, from = base + L::kRawAt + place * (uint32_t)L::kRawTile + (uint32_t)(r * D);
         ok = ok && mbar_wait(bar_raw_full(place), phase, abort_flag);
-        const int2 rows = const_cast<const int2*>(flags)[place];
+        int2 rows = const_cast<const int2*>(flags)[place];
+        const bool uneven = rows.x >= kUneven;
+        rows.x &= kUneven - 1;
         uint4 v[PER];
 #pragma unroll
         for (int p = 0; p < PER; ++p) v[p] = lds128(from + (uint32_t)(piece_of(p) * 16));
@@ -295,6 +351,16 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attention_tc_kernel(const _
         if (r < rows.x || r >= rows.y)
 #pragma unroll
           for (int p = 0; p < PER; ++p) v[p] = make_uint4(0u, 0u, 0u, 0u);
+        if (uneven) {                                                       // (the rows that see a NaN have it from set_seen_nan)
+          uint32_t nan = 0u;
+#pragma unroll
+          for (int p = 0; p < PER; ++p) {
+            uint32_t* const x = &v[p].x;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) { const uint32_t n = nan_codes(x[c]); nan |= n; x[c] &= ~(n * 0xffu); }
+          }
+          if (nan != 0u) *nan_flag = 1;
+        }
         __syncwarp();
         if (lane == 0) mbar_arrive(bar_raw_free(place));
         ok = ok && mbar_wait(bar_free(place), phase ^ 1u, abort_flag);
@@ -495,6 +561,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attention_tc_kernel(const _
       ok = __all_sync(0xffffffffu, ok);
       tc_fence_after();
       if (!ok) { *abort_flag = 1; break; }
+      if (__any_sync(0xffffffffu, *nan_flag != 0)) set_seen_nan<D>(a, keys_of_item(a, it), it.seq, it.head, it.page, it.n, on ? seen : KeyRange{0, 0}, to);
       const bool begun = it.page > it.first, goes_on = it.page + it.n < it.first + it.of, whole = !begun && !goes_on;
       if (l_run != l_run) m_run = INFINITY;                                // (goes on in other parts as infinity - infinity)
       if (on) {

@@ -71,6 +71,8 @@ __device__ __forceinline__ void codes_to_floats(uint32_t four, float (&x)[4]) {
   const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&l)), b = __half22float2(*reinterpret_cast<const __half2*>(&h));
   x[0] = a.x; x[1] = a.y; x[2] = b.x; x[3] = b.y;
 }
+// 1 in every byte that is NaN's code
+__device__ __forceinline__ uint32_t nan_codes(uint32_t four) { return ((four & 0x7f7f7f7fu) + 0x01010101u) >> 7 & 0x01010101u; }
 // nearest code, ties to the even one, magnitudes above 448 to 448, NaN to NaN
 __device__ __forceinline__ uint32_t float2_to_codes(float lo, float hi) {
   return (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(lo, hi), __NV_SATFINITE, __NV_E4M3);
