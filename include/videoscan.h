@@ -295,8 +295,8 @@ int vs_destroy_stream(vs_stream* h);
  * takes: rotary positions with several axes, a paged cache of 8-bit keys and values, attention over
  * it; and, beside vs_lm_head, what the logits say about given tokens.
  * These calls need no handle: the device is an argument (made current for the call and put back),
- * and they only enqueue work on `cuda_stream`, which must belong to it.  They keep no data between
- * calls, allocate nothing, and may be captured into a graph; calls on different streams are
+ * and they only enqueue work on `cuda_stream`, which must belong to it.  They keep nothing of the data
+ * between calls, allocate nothing, and may be captured into a graph; calls on different streams are
  * independent unless they share a workspace or write the same memory.  Integer arrays marked DEVICE
  * are read when the kernels run, so a captured call follows what they hold then.  Strides are in
  * elements; `dtype`: 0 = bf16, 1 = fp32. */
@@ -325,7 +325,9 @@ typedef struct {
 int vs_rope_axes(const vs_rope* rope, void* cuda_stream);
 
 /* A paged cache of 8-bit keys and values, the caller's memory.  Codes are e4m3 (largest 448); a
- * page's codes of one head share a scale 2^e, e in [-110, 120]: value = code * 2^e, exact in bf16. */
+ * page's codes of one head share a scale 2^e, e in [-110, 120]: value = code * 2^e, exact in bf16 and fp32
+ * while they hold it -- with e = 120, which rows beyond 1.75 * 2^127 (2.98e38) bring about, codes of 256 and
+ * more stand for 2^128 and more and read as infinity. */
 typedef struct {
   void*  k;                      /* DEVICE e4m3 [n_pages][n_kv_heads][VS_CACHE_PAGE][head_dim], 16-byte aligned */
   void*  v;                      /* ... values                                                       */
@@ -364,18 +366,18 @@ typedef struct {
 /* Appends rows to sequences, quantising them: a page's scale is the smallest power of two with every
  * finite magnitude written to it at most 448 of it, and not below the scale that the page had for the tokens
  * ahead of the rows; where rows raise it, the codes of those tokens are rounded once more at the new scale.  A row written to
- * the first place of a page starts the page afresh.  Nearest code, ties to even; infinities become +-448, NaN stays
+ * the first place of a page starts the page afresh.  Nearest code, ties to even; infinities become +-448 (of the scale), NaN stays
  * NaN.  Appending ends the sequence: codes behind its last row are left as they were and count for nothing.
  * No page may be written for two sequences of a call, or twice for one (pages that several sequences share
  * must be full); what such a page holds then is not defined. */
 int vs_cache_write(const vs_cache* cache, const vs_cache_rows* rows, void* cuda_stream);
 
-/* Reads rows back into k and v: the values that the codes stand for, exact in either dtype. */
+/* Reads rows back into k and v: the values that the codes stand for, exact in either dtype (infinity for 2^128 and more). */
 int vs_cache_read(const vs_cache* cache, const vs_cache_rows* rows, void* cuda_stream);
 
 /* Softmax attention of each sequence's rows over its tokens in the cache (Eq. 1, grouped KV heads):
- * row j of n stands at position tokens - n + j and sees the tokens that exist, with causal != 0 none
- * behind itself, with window > 0 only the last `window` up to itself.  A row that sees nothing gets zeros
+ * row j of n stands at position p = tokens - n + j and sees the tokens that exist, with causal != 0 none
+ * behind p, with window > 0 none at p - window or ahead of it (causal == 0: all behind itself all the same).  A row that sees nothing gets zeros
  * (and -inf in lse).  Tokens that a row does not see may hold anything, NaN too; a NaN value that it sees is its own in that element.
  * q:   DEVICE bf16 [n_rows][n_q_heads][head_dim], 16-byte aligned, strides multiples of 8;
  *      n_q_heads % n_kv_heads == 0, at most 8 query heads a KV head.
@@ -384,7 +386,7 @@ int vs_cache_read(const vs_cache* cache, const vs_cache_rows* rows, void* cuda_s
  *      strides multiples of 4; may be q itself (bf16, the same strides), but must not overlap it otherwise.
  *      Softmax weights are rounded to 11 bits, sums are fp32.
  * lse: DEVICE fp32 [n_rows][n_q_heads], log sum exp of a row's scores, or NULL: what joining the rows
- *      with those over other keys (the bank's, say) takes.
+ *      with a call's over other keys takes.
  * scale: of the scores, usually 1 / sqrt(head_dim).
  * workspace: DEVICE, at least vs_cache_attention_bytes, 256-byte aligned; its contents need not be kept
  *      between calls, but no two calls that may overlap can share it (calls of two host threads on one stream

@@ -82,3 +82,18 @@ def test_rows_joined_by_their_lse():
     l = torch.logaddexp(parts[0][1].double(), parts[1][1].double())
     o = sum(x.double() * (y.double() - l).exp()[..., None] for x, y in parts)
     assert float((l - lse).abs().max()) < 1e-4 and float((o - whole).abs().max()) < 1e-2
+
+
+def test_read_of_the_largest_values():
+    """What fp32 holds reads as the value of its code; codes of 256 and more at the largest scale stand for 2^128 and more."""
+    cache = binding.PageCache.empty(1, 1, 64)
+    x = torch.zeros(64, 1, 64, device="cuda")
+    values = [3.4e38, -3.4e38, 3.2e38, 3.0e38, 1.7e38, math.inf, -math.inf, 1e30]
+    x[0, 0, :8] = torch.tensor(values)
+    cache.write(ints([[0]]), ints([0]), x, x * 2.0 ** -1)
+    codes = cache.k.float()[0, 0, 0, :8]
+    assert float(cache.k_scale[0, 0]) == 2.0 ** 120 and codes.tolist() == [256, -256, 240, 224, 128, 448, -448, 0]
+    for dtype in (FP32, BF16):
+        k, v = cache.read(ints([[0]]), ints([0]), torch.empty_like(x, dtype=dtype), torch.empty_like(x, dtype=dtype))
+        assert k[0, 0, :8].tolist() == [math.inf, -math.inf, 240 * 2.0 ** 120, 224 * 2.0 ** 120, 2.0 ** 127, math.inf, -math.inf, 0]
+        assert bool(torch.isfinite(v[0, 0, :5]).all())
