@@ -525,39 +525,31 @@ __device__ __forceinline__ void join_items(const CacheAttnArgs& a, const int4* j
     if (lane == 0) store_lse(a, to, m, l);
   };
   if constexpr (W >= 8 * kJoinWarps) {
-    constexpr int P = 1, U = 4, groups = W / (P * kJoinWarps);          // columns of a warp, parts on their way at a time
+    constexpr int U = 4, groups = W / kJoinWarps;                       // parts on their way at a time
     if (2 * listed * groups >= (int)gridDim.x) {
       for (int at = (int)blockIdx.x; at < listed * groups; at += (int)gridDim.x) {
-        const int item = at / groups, col0 = (at % groups) * (P * kJoinWarps) + warp * P;
+        const int item = at / groups, col = (at % groups) * kJoinWarps + warp;
         const int4 j = sm.list[item];
         const int first = j.x - 1, last = sm.last[item];
-        if (col0 >= (j.w >> 16)) continue;                  // (the whole warp)
-        Sum s[P];
-#pragma unroll
-        for (int p = 0; p < P; ++p) s[p] = {-INFINITY, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
+        if (col >= (j.w >> 16)) continue;                   // (the whole warp)
+        Sum s = {-INFINITY, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
         bool wide = false;
 #pragma unroll 1
         for (int c0 = first; c0 <= last; c0 += U) {
-          float2 st[U][P];
-          float4 v[U][P];
+          float2 st[U];
+          float4 v[U];
 #pragma unroll
-          for (int i = 0; i < U; ++i)
+          for (int i = 0; i < U; ++i) {
+            const int c = min(c0 + i, last), place = c == first ? 1 : 0;
+            st[i] = c0 + i <= last ? part_stats<W, D>(parts, c, place)[col] : make_float2(-INFINITY, 0.f);
+            v[i] = c0 + i <= last && lane < D / 4 ? *reinterpret_cast<const float4*>(part_rows<W, D>(parts, c, place) + (size_t)col * D + 4 * lane)
+                                                  : make_float4(0.f, 0.f, 0.f, 0.f);
+          }
 #pragma unroll
-            for (int p = 0; p < P; ++p) {
-              const int c = min(c0 + i, last), place = c == first ? 1 : 0;
-              st[i][p] = c0 + i <= last ? part_stats<W, D>(parts, c, place)[col0 + p] : make_float2(-INFINITY, 0.f);
-              v[i][p] = c0 + i <= last && lane < D / 4 ? *reinterpret_cast<const float4*>(part_rows<W, D>(parts, c, place) + (size_t)(col0 + p) * D + 4 * lane)
-                                                       : make_float4(0.f, 0.f, 0.f, 0.f);
-            }
-#pragma unroll
-          for (int i = 0; i < U; ++i)
-#pragma unroll
-            for (int p = 0; p < P; ++p) { add_part(s[p], st[i][p], v[i][p]); wide = wide || shifted(st[i][p].y); }
+          for (int i = 0; i < U; ++i) { add_part(s, st[i], v[i]); wide = wide || shifted(st[i].y); }
         }
-#pragma unroll
-        for (int p = 0; p < P; ++p) if (wide) s[p].l = sum_of_parts<W, D>(parts, first, last, col0 + p, s[p].m);
-#pragma unroll
-        for (int p = 0; p < P; ++p) if (col0 + p < (j.w >> 16)) finish(j, col0 + p, s[p].m, s[p].l, s[p].o);
+        if (wide) s.l = sum_of_parts<W, D>(parts, first, last, col, s.m);
+        finish(j, col, s.m, s.l, s.o);
       }
       return;
     }
