@@ -429,7 +429,6 @@ struct JoinShared {
   int4 list[kFewCtas];                  // what the last CTA of an item noted
   int last[kFewCtas], count[(kFewCtas + 31) / 32];
   float2 st[kJoinWarps];
-  int wide[kJoinWarps];                 // whether a warp met a sum that is held times 2^-64
   float4 o[kJoinWarps][32];
 };
 // Parts of a row, up to 32 side by side: a lane knows one's reference and sum (on: there is one), and has four dims of each, which `get` gives
@@ -575,15 +574,16 @@ __device__ __forceinline__ void join_items(const CacheAttnArgs& a, const int4* j
       });
     }
     __syncthreads();                                        // (the round before has been read)
-    wide = __any_sync(0xffffffffu, wide);
-    if (lane == 0) { sm.st[warp] = make_float2(m, l); sm.wide[warp] = wide; }
+    if (__any_sync(0xffffffffu, wide)) l = -1.f;            // (to be summed up apart)
+    if (lane == 0) sm.st[warp] = make_float2(m, l);
     sm.o[warp][lane] = o;
     __syncthreads();
     if (warp != 0) continue;
     m = -INFINITY;
     o = make_float4(0.f, 0.f, 0.f, 0.f);
-    join_parts(kJoinWarps, lane < kJoinWarps, sm.st[lane & (kJoinWarps - 1)], m, l, o, [&](int i) { return sm.o[i][lane]; });
-    if (__any_sync(0xffffffffu, sm.wide[lane & (kJoinWarps - 1)] != 0)) l = sum_of_parts<W, D>(parts, first, last, col, m);
+    const float2 of_warp = sm.st[lane & (kJoinWarps - 1)];
+    join_parts(kJoinWarps, lane < kJoinWarps, of_warp, m, l, o, [&](int i) { return sm.o[i][lane]; });
+    if (__any_sync(0xffffffffu, shifted(of_warp.y))) l = sum_of_parts<W, D>(parts, first, last, col, m);
     finish(j, col, m, l, o);
   }
 }

@@ -102,7 +102,7 @@ __device__ __forceinline__ AttnRuns cut_units(const CacheAttnArgs& a, long long*
         most = max(most, n);
         u += rounded_up(n, whole);
       }
-      if (sub == 0) items += (int)min((long long)s.tiles * a.c.n_kv_heads, (long long)kMostWhole);
+      if (sub == 0) items = min(items + min(s.tiles, (int)kMostWhole) * a.c.n_kv_heads, (int)kMostWhole);      // (of 256 heads at most)
       return u * a.c.n_kv_heads;
     };
     // all units and items and the longest item, as far as the rule asks for them.  (An item has a unit at least: where the units are fewer than
@@ -112,7 +112,7 @@ __device__ __forceinline__ AttnRuns cut_units(const CacheAttnArgs& a, long long*
 #pragma unroll 1
     for (int i = lane >> shift; i < a.r.n_seqs; i += abreast) units = min(units + (uint32_t)min(units_of(i, 0, items, most), (long long)kMostWhole), kMostWhole);
     units = __reduce_add_sync(0xffffffffu, units);
-    items = max(__reduce_add_sync(0xffffffffu, min(items, 1 << 20)), 1);
+    items = max(__reduce_add_sync(0xffffffffu, items), 1);
     most = max(__reduce_max_sync(0xffffffffu, most), 1);
     int per_cta = 1;                                        // (of runs of `whole` units)
     if (units < kMostWhole) {

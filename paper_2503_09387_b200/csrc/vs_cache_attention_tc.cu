@@ -108,31 +108,33 @@ __device__ __forceinline__ uint4 lds128(uint32_t addr) {
   return v;
 }
 
-// Keys that any row of an item sees, and that all of them do.  (Both ends go up with the row.)
+// Keys [lo, hi) that any row of an item sees; of the pages that begin ahead of `ahead` or behind `behind` some rows see other keys than others.  (Both ends go
+// up with the row.)
 constexpr int kUneven = 256;
 struct ItemKeys {
-  int any_lo, all_lo, all_hi, any_hi;
-  // of a page: whether rows see different ones of its keys
-  __device__ __forceinline__ bool uneven(int key0) const { return (any_lo < all_lo && key0 < all_lo) || (all_hi < any_hi && key0 > all_hi - kPage); }
+  int lo, hi, ahead, behind;
+  __device__ __forceinline__ bool uneven(int key0) const { return key0 < ahead || key0 > behind; }
 };
 __device__ __forceinline__ ItemKeys keys_of_item(const CacheAttnArgs& a, const AttnItem& it) {
   const KeyRange first = keys_of(a, it.s, by_group(a, it.r0)), last = keys_of(a, it.s, by_group(a, it.r0 + it.n_cols - 1));
-  return {first.lo, last.lo, first.hi, last.hi};
+  return {first.lo, last.hi, first.lo < last.lo ? last.lo : 0, first.hi < last.hi ? first.hi - kPage : 0x7fffffff};
 }
 
 // The NaN of values that some rows of an item see and others do not.  The converters put zeros in their place; here, once the last product is
 // complete, every thread sets to NaN the dims of its row of O whose NaN the row sees.  It reads the pages in question once more.
 template <int D>
-__device__ __forceinline__ void set_seen_nan(const CacheAttnArgs& a, ItemKeys keys, int seq, int head, int page0, int n_pages, KeyRange seen, uint32_t to) {
+__device__ __forceinline__ void set_seen_nan(const CacheAttnArgs& a, const AttnItem& it, int col, uint32_t to) {
+  const ItemKeys keys = keys_of_item(a, it);
+  const KeyRange seen = col < it.n_cols ? keys_of(a, it.s, by_group(a, it.r0 + col)) : KeyRange{0, 0};
   uint32_t dims[D / 32];
 #pragma unroll
   for (int w = 0; w < D / 32; ++w) dims[w] = 0u;
-  for (int p = page0; p < page0 + n_pages; ++p) {
+  for (int p = it.page; p < it.page + it.n; ++p) {
     const int key0 = p * kPage;
     if (!keys.uneven(key0)) continue;
-    const int page = page_of(a.r, a.c.n_pages, seq, p);
+    const int page = page_of(a.r, a.c.n_pages, it.seq, p);
     if (page < 0) continue;
-    const uint8_t* const from = static_cast<const uint8_t*>(a.c.v) + ((size_t)page * a.c.n_kv_heads + head) * (size_t)(kPage * D);
+    const uint8_t* const from = static_cast<const uint8_t*>(a.c.v) + ((size_t)page * a.c.n_kv_heads + it.head) * (size_t)(kPage * D);
     for (int k = max(seen.lo - key0, 0); k < min(seen.hi - key0, kPage); ++k)
 #pragma unroll
       for (int w = 0; w < D / 32; ++w)
@@ -226,7 +228,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attention_tc_kernel(const _
             const uint8_t* const from = static_cast<const uint8_t*>(is_v ? a.c.v : a.c.k) + ((size_t)max(page, 0) * a.c.n_kv_heads + it.head) * (size_t)L::kRawTile;
             ok = mbar_wait(bar_raw_free(place), phase, abort_flag);
             if (ok) {
-              const_cast<int2*>(flags)[place] = page >= 0 ? make_int2(max(min(seen.any_lo - key0, kPage), 0) + (is_v && seen.uneven(key0) ? kUneven : 0), max(min(seen.any_hi - key0, kPage), 0)) : make_int2(0, 0);
+              const_cast<int2*>(flags)[place] = page >= 0 ? make_int2(max(min(seen.lo - key0, kPage), 0) + (is_v && seen.uneven(key0) ? kUneven : 0), max(min(seen.hi - key0, kPage), 0)) : make_int2(0, 0);
               if (page >= 0) {
                 mbar_arrive_expect_tx(bar_raw_full(place), (uint32_t)L::kRawTile);
                 bulk_load(base + L::kRawAt + place * (uint32_t)L::kRawTile, from, (uint32_t)L::kRawTile, bar_raw_full(place));
@@ -561,7 +563,8 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attention_tc_kernel(const _
       ok = __all_sync(0xffffffffu, ok);
       tc_fence_after();
       if (!ok) { *abort_flag = 1; break; }
-      if (__any_sync(0xffffffffu, *nan_flag != 0)) set_seen_nan<D>(a, keys_of_item(a, it), it.seq, it.head, it.page, it.n, on ? seen : KeyRange{0, 0}, to);
+      // (the item looked for once more: what it takes need not stay in registers for the rest of the time)
+      if (__any_sync(0xffffffffu, *nan_flag != 0)) set_seen_nan<D>(a, item_at<kWide>(a, before, runs, u - it.span, u_end, place_of), col, to);
       const bool begun = it.page > it.first, goes_on = it.page + it.n < it.first + it.of, whole = !begun && !goes_on;
       if (l_run != l_run) m_run = INFINITY;                                // (goes on in other parts as infinity - infinity)
       if (on) {
