@@ -469,7 +469,8 @@ class PageCache:
     def attend(self, page_table, lengths, q, out=None, lse=None, row_offsets=None, scale=None, causal=True, window=0, workspace=None,
                out_dtype=None):
         """Attention of q bf16 [n_rows, n_q_heads, head_dim] over each sequence's ``lengths[i]`` tokens, its rows counted in.
-        -> (out [n_rows, n_q_heads, head_dim], lse fp32 [n_rows, n_q_heads]).  ``out_dtype``: of a new ``out``, bf16 or fp32.  Without
+        -> (out [n_rows, n_q_heads, head_dim], lse fp32 [n_rows, n_q_heads]).  ``causal`` hides what lies behind a row, ``window`` > 0 what lies
+        ``window`` tokens or more ahead of it.  ``out_dtype``: of a new ``out``, bf16 or fp32.  Without
         ``workspace`` the cache keeps one for every stream it is used on; a call that is captured takes one from the graph's own memory, so
         that graphs replayed side by side share none (its status is then nobody's to read).  Several host threads may call it, on one stream too."""
         torch, index = _torch, self.device_index

@@ -16,7 +16,7 @@
 // ahead of their turn and placed so that both operands' fragments are read without bank conflicts: no barrier in the loop.
 // The work of all sequences is cut into equal runs of pages (cut_units): long and short sequences side by side leave no CTA idle.
 // Measured: sixteen sequences of 2000 to 65000 tokens, seven heads a group, 522 MB of codes: 90 us, 5.8 TB/s (89 % of what a copy reaches); one sequence of 13504:
-// 11.1 us from first to last -- 1.5 until the units are counted, 1 to the pages' numbers and first loads, 0.9 to their arrival, 1.7 for two steps, 1.2 for the
+// 11.3 us from first to last -- 1.5 until the units are counted, 1 to the pages' numbers and first loads, 0.9 to their arrival, 1.7 for two steps, 1.2 for the
 // warps' rows, then 3.3 for the join behind the launch's end.
 #include "vs_cache_attention.cuh"
 #include "vs_ptx.cuh"

@@ -14,8 +14,8 @@
 //
 // The codes go to fp16 once a page and CTA and serve 256 rows: fewer rows would convert more than they multiply, and fp8 operands would need the weights in
 // 8 bits, whose range of 2^18 loses a long row's many small ones beside one large one.  The query is held as fp16, exactly (see there).
-// Measured: 16600 pages and heads of four sequences' frames, 256 rows each: 179 us, 720 TFLOP/s; a page takes some 2000 clocks of a CTA, of which the tensor pipe is busy 41 %, the
-// exponentials' unit 42 %, the schedulers 49 %: a row's page is a chain -- scores out of tensor memory 250, maximum and votes 170, exponentials 1000,
+// Measured: 16600 pages and heads of four sequences' frames, 256 rows each: 183 us, 710 TFLOP/s; 13440 causal rows of one sequence 2.32 ms, 559; a page takes some 2000 clocks of a
+// CTA, of which the tensor pipe is busy 40 %, the exponentials' unit 41 %, the schedulers 49 %: a row's page is a chain -- scores out of tensor memory 250, maximum and votes 170, exponentials 1000,
 // back 40, barriers 450 -- of which a scheduler has two at a time, all that tensor memory has room for.  (Two threads a row 205 us, too many registers;
 // a part of the exponentials by a polynomial 183 against 182; a scheduler's two warps taking turns at the exponentials 194 against 185.)
 // All waits are bounded.

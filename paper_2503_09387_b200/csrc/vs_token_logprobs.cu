@@ -12,9 +12,10 @@
 // it hold any of the best k.  Their logits -- a few dozen threads' -- are read once more (they lie in L2), those that reach the bound collected and put in
 // order by counting.  (The bound by bisection, a barrier a bit, took 2 us more.)
 //
-// What bounds it: many rows, the instructions -- some thirteen a logit, two rows of 152064 take an SM 25 us in fp32 as in bf16 --; a row or two, the chain of loads,
-// maxima and the small sorts.  Few rows: the CTAs of a cluster share a row, and the first one joins their parts through shared memory; many: a
-// CTA a row.  Measured (fp32): 197 rows of 152064, five alternatives, 32 us (3.7 TB/s); 256 rows 33 (4.7 TB/s); one row 10.6, 7.2 without alternatives.
+// What bounds it: many rows, the SMs that have two of them (two rows of 152064 take one 25 us in fp32 as in bf16, 16 of them issue slots, some thirteen
+// instructions a logit; of 197 rows 49 SMs have two); a row or two, the chain of loads, maxima and the small sorts.  Few rows: the CTAs of a cluster share a row, and
+// the first one joins their parts through shared memory; many: a CTA a row.  Measured (fp32): 197 rows of 152064, five alternatives, 32 us (3.7 TB/s); 256 rows 33
+// (4.7 TB/s); one row 10.6, 7.2 without alternatives.
 #include "vs_operators.cuh"
 #include "vs_ptx.cuh"
 
